@@ -59,14 +59,15 @@ typedef enum {
   EB_POLICY_ALL = 3
 } eb_policy;
 
-enum { EB_MAX_MB = 16, EB_MAX_D = 16, EB_MAX_E = 256, EB_MAX_K = 8, EB_MAX_S = 8 };
+enum { EB_MAX_MB = 16, EB_MAX_D = 16, EB_MAX_E = 256, EB_MAX_K = 8, EB_MAX_S = 8, EB_MAX_ROUTER_GROUPS = 32 };
 
 /* Length of the int32 `step_meta` array written by eb_permute:
  *   [0] R = rows of this step, [1] G = groups, [2] number of active layers,
  *   [3 .. 3+D] first group of every virtual device (D+1 entries),
  *   [EB_META_LEN-1] routing indices outside [0, E) met in topk_idx: each is skipped (its slot gets
- *   pos = -1 and no row, it is never used as an index) and counted here; always 0 for indices
- *   written by eb_route.  The entries in between are unused. */
+ *   pos = -1 and no row, it is never used as an index) and counted here; 0 for indices
+ *   written by eb_route, unless a router with masked experts (eb_router) left slots empty (-1).  The
+ *   entries in between are unused. */
 enum { EB_META_LEN = 32 };
 
 typedef struct {
@@ -94,13 +95,35 @@ typedef struct {
   int64_t util_den;    /* D * max_d joint_load[d]  (Eq. 3 for this step; 0 means no work) */
 } eb_sched_result;
 
+/* Gating by scores, an alternative to eb_route's softmax top-k on the logits z of a token:
+ *   s_e = sigmoid(z_e) or softmax(z)_e;  c_e = s_e + bias[layer][e], what the choice goes by;
+ *   the experts form n_group groups of E / n_group neighbours; a group is worth its best c_e (group_top 1) or the sum of its
+ *   best two (group_top 2; of one where there is only one); the topk_group best groups stay (ties: lower group first);
+ *   the K best c_e of these are chosen, in that order (ties: lower index first), with weights scale * s_e, divided by the sum of
+ *   the chosen s_e first if the context renormalises (renorm_topk).
+ * Choices are made as by 64-bit scores: no near value is mistaken for a tie, or for the larger one.  A logit of -inf or NaN
+ * (and a bias of -inf or NaN) masks its expert: it is never chosen and counts for no group.  Slots for which no expert is left get
+ * index -1 and weight 0: no row in the dispatch, nothing in the loads and in the aggregation.  A logit of +inf counts as the
+ * largest float. */
+typedef enum { EB_SCORE_SOFTMAX = 0, EB_SCORE_SIGMOID = 1 } eb_score;
+typedef enum { EB_TYPE_F32 = 0, EB_TYPE_BF16 = 1 } eb_type;
+typedef struct {
+  int32_t score;      /* eb_score */
+  int32_t n_group;    /* divides E, at most EB_MAX_ROUTER_GROUPS; 1: no groups */
+  int32_t topk_group; /* groups that stay, 1 .. n_group; they hold at least K experts */
+  int32_t group_top;  /* 1 or 2 */
+  float scale;        /* factor on the weights, positive */
+  const float* bias;  /* device f32 [L][E], borrowed (as weights are); NULL: none */
+} eb_router;
+
 /* Device buffers of one step, for eb_step / eb_step_host.  Sizes in elements:
  *   logits f32 [max_tokens, E]; x bf16 [max_tokens, H]; topk_idx i32 [max_tokens, K];
  *   topk_w f32 [max_tokens, K]; mb_load i32 [EB_MAX_MB, D]; mb_cnt i32 [EB_MAX_MB, E];
  *   sched: one eb_sched_result; group_off i32 [eb_groups_capacity + 1];
  *   group_w i32 [eb_groups_capacity]; row_src i32 [eb_rows_capacity];
  *   pos i32 [max_tokens, K + S]; xp, yp bf16 [eb_rows_capacity, H]; step_meta i32 [EB_META_LEN];
- *   out bf16 [max_tokens, H]. */
+ *   out bf16 [max_tokens, H].  With 8-bit weights bound, xp holds what eb_permute_fp8 writes: the rows xq, and
+ *   their scales xs from byte eb_rows_capacity * H on. */
 typedef struct {
   float* logits;
   void* x;
@@ -156,6 +179,16 @@ int32_t eb_groups_capacity(const eb_ctx* ctx); /* EB_MAX_MB * (E + D * S) */
 eb_status eb_route(eb_ctx* ctx, void* stream, const eb_batch* batch, uint32_t route_mask,
                    const float* logits, int32_t* topk_idx, float* topk_w,
                    int32_t* mb_load, int32_t* mb_cnt);
+
+/* The same by an eb_router (host; copied at call time).  logits f32 or bf16, row_stride elements from one token's to the next (at least
+ * E), aligned to their type.  Written are the same outputs in the same places. */
+eb_status eb_route_scored(eb_ctx* ctx, void* stream, const eb_batch* batch, uint32_t route_mask, const eb_router* router,
+                          const void* logits, eb_type type, int64_t row_stride, int32_t* topk_idx, float* topk_w,
+                          int32_t* mb_load, int32_t* mb_cnt);
+
+/* From now on eb_route, eb_step and the calls around it gate by this router (copied; its bias is borrowed until the next
+ * eb_set_router); NULL: by softmax top-k again, as after eb_create.  Graphs keep the router that they were captured with. */
+eb_status eb_set_router(eb_ctx* ctx, const eb_router* router);
 
 /* Schedule(S, m) of Algorithm 1 on the routed loads.  If the pool has at most m members all
  * run.  MaxUtil scores every subset with at least m members by sum(W) / (D * max(W)), W the
@@ -216,9 +249,41 @@ eb_status eb_expert_ffn_device(eb_ctx* ctx, void* stream, const void* xp, const 
                                const int32_t* group_w, const int32_t* step_meta, void* yp,
                                int32_t device);
 
+/* ---- 8-bit weights -------------------------------------------------------------------------
+ * e4m3 values with one f32 scale per block: of 128 x 128 elements of a weight matrix, of 128 elements of a token's row (the last
+ * blocks of a row or column hold what is left).  A block's scale is m / 448, m its largest magnitude, its values are
+ * v * 448 / m rounded to nearest even (0 for a block of zeros).  A block with an infinity or NaN gets the scale NaN, and so
+ * does everything made from it.  H and I are multiples of 16. */
+
+/* Lays the context out for 8-bit weights as well.  After eb_create, before eb_workspace_bytes and eb_set_workspace (a workspace set before
+ * has to be set again: it is larger now).  EB_ERR_UNSUPPORTED if H or I is no multiple of 16. */
+eb_status eb_enable_fp8(eb_ctx* ctx);
+
+/* bf16 matrices w [n_mat][rows][cols] to q (e4m3, same shape) and scale f32 [n_mat][ceil(rows / 128)][ceil(cols / 128)].  cols % 8 == 0; any
+ * context of the device will do. */
+eb_status eb_quantize_weights(eb_ctx* ctx, void* stream, const void* w, int32_t n_mat, int32_t rows, int32_t cols, void* q, float* scale);
+
+/* Expert weights in the layout of eb_bind_weights as e4m3, with scales f32 [L][E+S][ceil(I/128)][ceil(H/128)] (gate, up) and
+ * [L][E+S][ceil(H/128)][ceil(I/128)] (down), 16-byte aligned, borrowed.  eb_step and the calls around it use the weights bound last;
+ * eb_expert_ffn_grouped the last bf16 ones, eb_expert_ffn_grouped_fp8 the last 8-bit ones. */
+eb_status eb_bind_weights_fp8(eb_ctx* ctx, const void* w_gate, const float* s_gate, const void* w_up, const float* s_up,
+                              const void* w_down, const float* s_down);
+
+/* eb_permute with the rows quantised: xq e4m3 [eb_rows_capacity, H], xs f32 [eb_rows_capacity, ceil(H/128)]; x is read, and a row
+ * quantised, once for all its K + S places. */
+eb_status eb_permute_fp8(eb_ctx* ctx, void* stream, const eb_batch* batch, const eb_sched_result* d_res, const void* x,
+                         const int32_t* topk_idx, int32_t* group_off, int32_t* group_w, int32_t* row_src, int32_t* pos,
+                         void* xq, float* xs, int32_t* step_meta);
+
+/* eb_expert_ffn_grouped (device < 0; else eb_expert_ffn_device) on 8-bit rows and weights: products of e4m3 values summed in fp32 over
+ * blocks of 128, the blocks' sums times both scales added up in fp32, silu(gate) * up quantised like a row (blocks of 128 of
+ * the I outputs; one whose largest magnitude is below 2^-110 counts as zeros), yp bf16.  xq, xs: as eb_permute_fp8 leaves them. */
+eb_status eb_expert_ffn_grouped_fp8(eb_ctx* ctx, void* stream, const void* xq, const float* xs, const int32_t* group_off,
+                                    const int32_t* group_w, const int32_t* step_meta, void* yp, int32_t device);
+
 /* Weighted aggregation, Eq. 1: out[t] = sum_k topk_w[t][k] * yp[pos[t][k]] + sum_s yp[pos[t][K+s]]
  * in fp32, k ascending then s, rounded to bf16.  Rows of tokens whose micro-batch did not run
- * are left untouched.  No residual is added. */
+ * are left untouched; a slot without a row (pos -1) adds nothing.  No residual is added. */
 eb_status eb_combine(eb_ctx* ctx, void* stream, const eb_batch* batch, const eb_sched_result* d_res,
                      const void* yp, const int32_t* pos, const float* topk_w, void* out);
 

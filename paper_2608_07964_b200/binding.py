@@ -7,6 +7,7 @@ There is no CPU fallback: loading fails loudly when the library is missing.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence
@@ -21,6 +22,10 @@ EB_MAX_D = 16
 EB_META_LEN = 32
 EB_HOST_SLOTS = 4
 
+SCORES = {"softmax": 0, "sigmoid": 1}
+BLOCK = 128                # elements of a scale block of 8-bit rows and weights
+FP8 = torch.float8_e4m3fn
+
 POLICY_MAXUTIL, POLICY_CUMUTIL, POLICY_DIFFPEAK, POLICY_ALL = 0, 1, 2, 3
 
 
@@ -32,6 +37,10 @@ class EbConfig(C.Structure):
 class EbBatch(C.Structure):
     _fields_ = [("n_mb", C.c_int32), ("tok_off", C.POINTER(C.c_int32)), ("layer", C.POINTER(C.c_int32)),
                 ("pool_mask", C.c_uint32)]
+
+
+class EbRouter(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("score", "n_group", "topk_group", "group_top")] + [("scale", C.c_float), ("bias", C.c_void_p)]
 
 
 class EbSchedResult(C.Structure):
@@ -48,7 +57,8 @@ class EbStepBuffers(C.Structure):
 SYMBOLS = ["eb_copy", "eb_watch_schedule", "eb_schedule_wait", "eb_create", "eb_destroy", "eb_bind_weights", "eb_workspace_bytes", "eb_set_workspace",
            "eb_rows_capacity", "eb_groups_capacity", "eb_route", "eb_schedule", "eb_permute",
            "eb_expert_ffn_grouped", "eb_expert_ffn_device", "eb_combine", "eb_combine_residual", "eb_step", "eb_step_host",
-           "eb_step_host_submit", "eb_step_host_wait",
+           "eb_step_host_submit", "eb_step_host_wait", "eb_route_scored", "eb_set_router", "eb_enable_fp8", "eb_quantize_weights",
+           "eb_bind_weights_fp8", "eb_permute_fp8", "eb_expert_ffn_grouped_fp8",
            "eb_permute_noalloc", "eb_selftest_bounded_wait", "eb_check_permutation", "eb_check_workspace_guards",
            "eb_device_status", "eb_num_kernels", "eb_kernel_name", "eb_set_timing", "eb_kernel_ms",
            "eb_launch_count", "eb_status_string", "eb_last_error"]
@@ -79,6 +89,13 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.eb_rows_capacity.argtypes = [vp]
     lib.eb_groups_capacity.argtypes = [vp]
     lib.eb_route.argtypes = [vp, vp, C.POINTER(EbBatch), u32, vp, vp, vp, vp, vp]
+    lib.eb_route_scored.argtypes = [vp, vp, C.POINTER(EbBatch), u32, C.POINTER(EbRouter), vp, i32, C.c_int64, vp, vp, vp, vp]
+    lib.eb_set_router.argtypes = [vp, C.POINTER(EbRouter)]
+    lib.eb_enable_fp8.argtypes = [vp]
+    lib.eb_quantize_weights.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
+    lib.eb_bind_weights_fp8.argtypes = [vp] * 7
+    lib.eb_permute_fp8.argtypes = [vp, vp, C.POINTER(EbBatch), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.eb_expert_ffn_grouped_fp8.argtypes = [vp] * 8 + [i32]
     lib.eb_schedule.argtypes = [vp, vp, C.POINTER(EbBatch), i32, i32, vp, vp, vp]
     lib.eb_copy.argtypes = [vp, vp, vp, vp, C.c_size_t]
     lib.eb_watch_schedule.argtypes = [vp, u32]
@@ -159,11 +176,25 @@ class Batch:
         return self.tok_off[-1]
 
 
+class Router:
+    """Gating by scores, groups of experts and a balance bias (eb_router in eb.h): `score` "softmax" or "sigmoid"; `bias` f32 [L, E] on the
+    device, for the choice alone, or None; `n_group` groups of which the `topk_group` best stay, each worth its best
+    (`group_top` 1) or its best two (2) biased scores; `scale` on the weights."""
+
+    def __init__(self, score: str = "softmax", bias: Optional[torch.Tensor] = None, n_group: int = 1, topk_group: int = 1, group_top: int = 1,
+                 scale: float = 1.0):
+        assert score in SCORES, score
+        assert bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.is_contiguous())
+        self.score, self.bias, self.n_group, self.topk_group, self.group_top, self.scale = score, bias, n_group, topk_group, group_top, scale
+        self.c = EbRouter(SCORES[score], n_group, topk_group, group_top, scale, _ptr(bias))
+
+
 class MoEStep:
     """Owns an eb context plus the device buffers of one step (allocated with PyTorch)."""
 
     def __init__(self, L, E, K, S, H, I, D, expert_to_device: Sequence[int], max_tokens: int,
-                 renorm_topk: int = 1, device: str = "cuda:0", lib_path: Optional[str] = None):
+                 renorm_topk: int = 1, device: str = "cuda:0", lib_path: Optional[str] = None, fp8: bool = False):
+        """`fp8`: laid out for 8-bit weights too (bind_weights_fp8, eb_permute_fp8, eb_expert_ffn_grouped_fp8)."""
         self.lib = load_library(lib_path)
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
@@ -174,6 +205,9 @@ class MoEStep:
         h = C.c_void_p()
         self._check(self.lib.eb_create(C.byref(cfg), C.byref(h)), ctx=None)
         self.ctx = h
+        self.fp8 = fp8
+        if fp8:
+            self._check(self.lib.eb_enable_fp8(self.ctx))
         self.rows_cap = self.lib.eb_rows_capacity(self.ctx)
         self.groups_cap = self.lib.eb_groups_capacity(self.ctx)
         nbytes = self.lib.eb_workspace_bytes(self.ctx)
@@ -203,7 +237,12 @@ class MoEStep:
         self.bufs_inplace = EbStepBuffers(*[t.data_ptr() for t in (
             self.logits, self.x, self.topk_idx, self.topk_w, self.mb_load, self.mb_cnt, self.sched, self.group_off,
             self.group_w, self.row_src, self.pos, self.xp, self.yp, self.step_meta, self.x)], self.x.data_ptr())
-        self._weights = None
+        if fp8:   # the rows of a dispatch as e4m3 values and their scales, in the memory of xp
+            raw = self.xp.view(torch.uint8).view(-1)
+            n, blocks = self.rows_cap * H, -(-H // BLOCK)
+            self.xq = raw[:n].view(FP8).view(self.rows_cap, H)
+            self.xs = raw[n:n + 4 * self.rows_cap * blocks].view(f32).view(self.rows_cap, blocks)
+        self._weights = self._weights8 = self._router = None
         self._waited = 0          # ticket of the last schedule_wait
 
     # -- helpers -------------------------------------------------------------------------------
@@ -234,12 +273,53 @@ class MoEStep:
         self._weights = (w_gate, w_up, w_down)
         self._check(self.lib.eb_bind_weights(self.ctx, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()))
 
+    def quantize_weights(self, w: torch.Tensor):
+        """bf16 matrices [..., rows, cols] as e4m3 values and f32 scales [..., ceil(rows / 128), ceil(cols / 128)]."""
+        assert w.device == self.logits.device and w.dtype == torch.bfloat16 and w.is_contiguous() and w.dim() >= 2
+        *lead, rows, cols = w.shape
+        q = torch.empty(w.shape, dtype=FP8, device=self.dev)
+        scale = torch.empty((*lead, -(-rows // BLOCK), -(-cols // BLOCK)), dtype=torch.float32, device=self.dev)
+        n = math.prod(lead)
+        self._check(self.lib.eb_quantize_weights(self.ctx, _stream(), w.data_ptr(), n, rows, cols, q.data_ptr(), scale.data_ptr()))
+        return q, scale
+
+    def bind_weights_fp8(self, w_gate, s_gate, w_up, s_up, w_down, s_down):
+        """Expert weights as e4m3 values in the layout of `bind_weights`, each with its scales [L, E + S, rows / 128, cols / 128] (rounded up)."""
+        n, hb, ib = self.E + self.S, -(-self.H // BLOCK), -(-self.I // BLOCK)
+        for w in (w_gate, w_up, w_down):
+            assert w.device == self.logits.device and w.dtype == FP8 and w.is_contiguous()
+        for s in (s_gate, s_up, s_down):
+            assert s.device == self.logits.device and s.dtype == torch.float32 and s.is_contiguous()
+        assert tuple(w_gate.shape) == (self.L, n, self.I, self.H) == tuple(w_up.shape)
+        assert tuple(w_down.shape) == (self.L, n, self.H, self.I)
+        assert tuple(s_gate.shape) == (self.L, n, ib, hb) == tuple(s_up.shape) and tuple(s_down.shape) == (self.L, n, hb, ib)
+        self._weights8 = (w_gate, s_gate, w_up, s_up, w_down, s_down)
+        self._check(self.lib.eb_bind_weights_fp8(self.ctx, *[t.data_ptr() for t in self._weights8]))
+
+    def set_router(self, router: Optional[Router] = None):
+        """From now on eb_route and whole steps gate by `router`; None: by softmax top-k again."""
+        if router is not None and router.bias is not None:
+            assert router.bias.device == self.logits.device and tuple(router.bias.shape) == (self.L, self.E)
+        self._check(self.lib.eb_set_router(self.ctx, None if router is None else C.byref(router.c)))
+        self._router = router   # its bias is borrowed
+
     # -- the five calls ------------------------------------------------------------------------
     def eb_route(self, batch: Batch, route_mask: Optional[int] = None, logits: Optional[torch.Tensor] = None):
         lg = self.logits if logits is None else logits
         rm = ((1 << batch.n_mb) - 1) if route_mask is None else route_mask
         self._check(self.lib.eb_route(self.ctx, _stream(), C.byref(batch.c), rm, lg.data_ptr(), self.topk_idx.data_ptr(),
                                       self.topk_w.data_ptr(), self.mb_load.data_ptr(), self.mb_cnt.data_ptr()))
+
+    def eb_route_scored(self, batch: Batch, router: Router, logits: Optional[torch.Tensor] = None, route_mask: Optional[int] = None):
+        """eb_route by `router`; logits f32 or bf16 [T, E], rows of any stride."""
+        lg = self.logits if logits is None else logits
+        rm = ((1 << batch.n_mb) - 1) if route_mask is None else route_mask
+        assert lg.device == self.logits.device and lg.dim() == 2 and lg.shape[1] == self.E and lg.shape[0] >= batch.n_tok and lg.dtype in (torch.float32, torch.bfloat16)
+        assert (self.E == 1 or lg.stride(1) == 1) and (lg.shape[0] <= 1 or lg.stride(0) >= self.E)
+        assert router.bias is None or (router.bias.device == self.logits.device and tuple(router.bias.shape) == (self.L, self.E))
+        self._check(self.lib.eb_route_scored(self.ctx, _stream(), C.byref(batch.c), rm, C.byref(router.c), lg.data_ptr(), int(lg.dtype == torch.bfloat16),
+                                             max(lg.stride(0), self.E), self.topk_idx.data_ptr(), self.topk_w.data_ptr(), self.mb_load.data_ptr(),
+                                             self.mb_cnt.data_ptr()))
 
     def eb_schedule(self, batch: Batch, m: int, policy: int = POLICY_MAXUTIL, to_host: bool = False,
                     mb_load: Optional[torch.Tensor] = None) -> Optional[Dict]:
@@ -309,6 +389,21 @@ class MoEStep:
                                         self.topk_idx.data_ptr(), self.group_off.data_ptr(), self.group_w.data_ptr(),
                                         self.row_src.data_ptr(), self.pos.data_ptr(), self.xp.data_ptr(),
                                         self.step_meta.data_ptr()))
+
+    def eb_permute_fp8(self, batch: Batch, x: Optional[torch.Tensor] = None):
+        """eb_permute with the rows quantised, to self.xq and self.xs (in the memory of self.xp)."""
+        assert self.fp8, "MoEStep(..., fp8=True)"
+        xx = self.x if x is None else x
+        self._check(self.lib.eb_permute_fp8(self.ctx, _stream(), C.byref(batch.c), self.sched.data_ptr(), xx.data_ptr(), self.topk_idx.data_ptr(),
+                                            self.group_off.data_ptr(), self.group_w.data_ptr(), self.row_src.data_ptr(), self.pos.data_ptr(),
+                                            self.xq.data_ptr(), self.xs.data_ptr(), self.step_meta.data_ptr()))
+
+    def eb_expert_ffn_grouped_fp8(self, device: Optional[int] = None):
+        """The expert pass over self.xq and self.xs with the 8-bit weights bound last, to self.yp."""
+        assert self.fp8, "MoEStep(..., fp8=True)"
+        self._check(self.lib.eb_expert_ffn_grouped_fp8(self.ctx, _stream(), self.xq.data_ptr(), self.xs.data_ptr(), self.group_off.data_ptr(),
+                                                       self.group_w.data_ptr(), self.step_meta.data_ptr(), self.yp.data_ptr(),
+                                                       -1 if device is None else device))
 
     def eb_expert_ffn_grouped(self, device: Optional[int] = None):
         if device is None:
@@ -458,7 +553,7 @@ def _sched_dict(h: EbSchedResult, D: int) -> Dict:
                 joint_load=list(h.joint_load)[:D], util_num=h.util_num, util_den=h.util_den)
 
 
-def from_workload(wl, device: str = "cuda:0", max_tokens: Optional[int] = None) -> MoEStep:
+def from_workload(wl, device: str = "cuda:0", max_tokens: Optional[int] = None, fp8: bool = False) -> MoEStep:
     """Context + buffers sized for a synthetic workload description (see synth.Workload)."""
     return MoEStep(wl.L, wl.E, wl.K, wl.S, wl.H, wl.I, wl.D, wl.expert_to_device(),
-                   max_tokens or wl.T_tot, wl.renorm_topk, device)
+                   max_tokens or wl.T_tot, wl.renorm_topk, device, fp8=fp8)

@@ -86,7 +86,7 @@ static size_t carve(eb_ctx* c, char* base) {
   };
   c->max_chunks = (g.max_tokens + 31) / 32 + EB_MAX_MB;
   int rows = ebi_rows_cap(c), gcap = ebi_groups_cap(c);
-  c->max_tiles = rows / 256 + gcap;                    // a group of r rows has ceil(r / 256) tiles
+  c->max_tiles = rows / (c->fp8 ? 128 : 256) + gcap;   // a group of r rows has ceil(r / 256) tiles, ceil(r / 128) with 8-bit weights
   c->max_work = c->max_tiles * ((g.I + 255) / 256 + (g.H + 511) / 512);   // 256 outputs per gate/up tile, 512 per down tile
   c->chunk_hist = (int32_t*)take(sizeof(int32_t) * (size_t)c->max_chunks * g.E);
   c->chunk_base = (int32_t*)take(sizeof(int32_t) * (size_t)c->max_chunks * g.E);
@@ -103,7 +103,8 @@ static size_t carve(eb_ctx* c, char* base) {
   c->work = take(32 * (size_t)c->max_work);
   c->tile_ready = (int32_t*)take(sizeof(int32_t) * (size_t)c->max_tiles);
   c->slots = (int2*)take(sizeof(int2) * 16 * (size_t)c->max_tiles);
-  c->act = (bf16*)take(sizeof(bf16) * (size_t)rows * g.I);
+  c->act = (bf16*)take(sizeof(bf16) * (size_t)rows * g.I);   // with 8-bit weights bytes, in the first half
+  if (c->fp8) c->act_scale = (float*)take(sizeof(float) * (size_t)rows * ebi_blocks(g.I));
   return off;
 }
 
@@ -201,6 +202,37 @@ extern "C" eb_status eb_bind_weights(eb_ctx* c, const void* w_gate, const void* 
   c->w_down = (const bf16*)w_down;
   eb_status s = ebi_ffn_bind(c);
   if (s != EB_OK) c->w_gate = c->w_up = c->w_down = nullptr;
+  else c->use_fp8 = false;
+  return s;
+}
+
+extern "C" eb_status eb_enable_fp8(eb_ctx* c) {
+  if (!c) return EB_ERR_INVALID_ARG;
+  if (c->cfg.H % 16 || c->cfg.I % 16) return ebi_fail(c, EB_ERR_UNSUPPORTED, "8-bit weights need H % 16 == 0 and I % 16 == 0");
+  if (c->fp8) return EB_OK;
+  c->fp8 = true;
+  c->ws = nullptr;   // the workspace is larger now
+  c->ws_bytes = 0;
+  carve(c, nullptr);
+  return EB_OK;
+}
+
+extern "C" eb_status eb_bind_weights_fp8(eb_ctx* c, const void* w_gate, const float* s_gate, const void* w_up, const float* s_up,
+                                         const void* w_down, const float* s_down) {
+  if (!c) return EB_ERR_INVALID_ARG;
+  if (!c->fp8) return ebi_fail(c, EB_ERR_INVALID_ARG, "eb_enable_fp8 first");
+  if (!w_gate || !w_up || !w_down || !s_gate || !s_up || !s_down) return ebi_fail(c, EB_ERR_INVALID_ARG, "null weights");
+  if (!ebi_aligned16(w_gate) || !ebi_aligned16(w_up) || !ebi_aligned16(w_down) || !ebi_aligned16(s_gate) || !ebi_aligned16(s_up) || !ebi_aligned16(s_down))
+    return ebi_fail(c, EB_ERR_INVALID_ARG, "weights must be 16-byte aligned");
+  c->w8_gate = w_gate;
+  c->w8_up = w_up;
+  c->w8_down = w_down;
+  c->s8_gate = s_gate;
+  c->s8_up = s_up;
+  c->s8_down = s_down;
+  eb_status s = ebi_ffn8_bind(c);
+  if (s != EB_OK) c->w8_gate = c->w8_up = c->w8_down = nullptr;
+  else c->use_fp8 = true;
   return s;
 }
 
@@ -208,6 +240,7 @@ extern "C" size_t eb_workspace_bytes(const eb_ctx* c) {
   if (!c) return 0;
   eb_ctx tmp;
   tmp.cfg = c->cfg;
+  tmp.fp8 = c->fp8;
   return carve(&tmp, nullptr);
 }
 
@@ -241,6 +274,13 @@ extern "C" eb_status eb_expert_ffn_device(eb_ctx* c, void* stream, const void* x
   return ebi_ffn_run(c, (cudaStream_t)stream, xp, group_off, group_w, step_meta, yp, device);
 }
 
+extern "C" eb_status eb_expert_ffn_grouped_fp8(eb_ctx* c, void* stream, const void* xq, const float* xs, const int32_t* group_off,
+                                               const int32_t* group_w, const int32_t* step_meta, void* yp, int32_t device) {
+  if (!c) return EB_ERR_INVALID_ARG;
+  if (device >= c->cfg.D) return ebi_fail(c, EB_ERR_INVALID_ARG, "device out of range");
+  return ebi_ffn8_run(c, (cudaStream_t)stream, xq, xs, group_off, group_w, step_meta, yp, device < 0 ? -1 : device);
+}
+
 static eb_status check_buffers(eb_ctx* c, const eb_step_buffers* b) {
   if (!b) return ebi_fail(c, EB_ERR_INVALID_ARG, "null buffers");
   const void* p[] = {b->logits, b->x, b->topk_idx, b->topk_w, b->mb_load, b->mb_cnt, b->sched, b->group_off,
@@ -263,7 +303,9 @@ extern "C" eb_status eb_step(eb_ctx* c, void* stream, const eb_batch* batch, uin
   if (!c->ws) return ebi_fail(c, EB_ERR_WORKSPACE, "no workspace set");
   cudaStream_t st = (cudaStream_t)stream;
   if ((s = ebi_front_run(c, st, bp, batch->pool_mask, route_mask, m, policy, b)) != EB_OK) return s;
-  if ((s = ebi_ffn_run(c, st, b->xp, b->group_off, b->group_w, b->step_meta, b->yp, -1, true)) != EB_OK) return s;
+  s = c->use_fp8 ? ebi_ffn8_run(c, st, b->xp, ebi_row_scales(c, b->xp), b->group_off, b->group_w, b->step_meta, b->yp, -1, true)
+                 : ebi_ffn_run(c, st, b->xp, b->group_off, b->group_w, b->step_meta, b->yp, -1, true);
+  if (s != EB_OK) return s;
   if (!ebi_aligned16(b->residual)) return ebi_fail(c, EB_ERR_INVALID_ARG, "residual not 16-byte aligned");
   return eb_combine_residual(c, stream, batch, b->sched, b->yp, b->pos, b->topk_w, b->residual, b->out);
 }

@@ -29,8 +29,9 @@ __device__ __forceinline__ void fma8(float* acc, const uint4& v, float w) {
 
 template <int KS>
 __global__ void __launch_bounds__(kThreads)
-combine_kernel(int n_tok, int H, int K, int team, const uint4* __restrict__ yp, const int32_t* __restrict__ pos,
+combine_kernel(const __grid_constant__ BatchParams bp, const eb_sched_result* __restrict__ res, int H, int K, int team, const uint4* __restrict__ yp, const int32_t* __restrict__ pos,
                const float* __restrict__ topk_w, const uint4* residual, uint4* out) {   // residual may be `out` itself
+  const int n_tok = bp.n_tok;
   const int t = blockIdx.x * (kThreads / team) + threadIdx.x / team;   // team >= 32: a warp serves one token
   const int lane = threadIdx.x & 31;
   // by one warp per token: hints of all eight warps, and for the output row too, took 4 x 4096 tokens of 2048 elements from 26.5 us
@@ -40,8 +41,12 @@ combine_kernel(int n_tok, int H, int K, int team, const uint4* __restrict__ yp, 
   if (t >= n_tok) return;
   // lane s fetches slot s once per warp; the values are broadcast with shuffles
   const int my_pos = lane < KS ? pos[(size_t)t * KS + lane] : -1;
-  const float my_w = lane < K ? topk_w[(size_t)t * K + lane] : 1.0f;
-  if (__shfl_sync(0xffffffffu, my_pos, 0) < 0) return;  // micro-batch did not run: row untouched
+  const float my_w = lane < K ? (my_pos >= 0 ? topk_w[(size_t)t * K + lane] : 0.f) : 1.0f;   // a slot without a row adds 0 whatever its weight
+  if (!__any_sync(0xffffffffu, my_pos >= 0)) {   // no row at all
+    int j = 0;
+    while (j + 1 < bp.n_mb && t >= bp.tok_off[j + 1]) ++j;
+    if (!((res->run_mask >> j) & 1u)) return;    // micro-batch did not run: row untouched; else the sum is 0
+  }
   const int vec = H / 8;
   int p[KS];
   float w[KS];
@@ -76,7 +81,7 @@ combine_kernel(int n_tok, int H, int K, int team, const uint4* __restrict__ yp, 
   }
 }
 
-typedef void (*combine_fn)(int, int, int, int, const uint4*, const int32_t*, const float*, const uint4*, uint4*);
+typedef void (*combine_fn)(BatchParams, const eb_sched_result*, int, int, int, const uint4*, const int32_t*, const float*, const uint4*, uint4*);
 
 // kernel for every slot count 1 .. kMaxSlots (entry 0 unused)
 template <int... Is>
@@ -109,7 +114,7 @@ extern "C" eb_status eb_combine_residual(eb_ctx* c, void* stream, const eb_batch
   KernelTimer timer(c, EBK_COMBINE, st);
   const int vec = c->cfg.H / 8;
   const int team = vec <= 32 ? 32 : vec <= 64 ? 64 : vec <= 128 ? 128 : 256, tpb = kThreads / team;
-  ebi_launch(table[KS], dim3((bp.n_tok + tpb - 1) / tpb), dim3(kThreads), 0, st, bp.n_tok, c->cfg.H, c->cfg.K, team,
+  ebi_launch(table[KS], dim3((bp.n_tok + tpb - 1) / tpb), dim3(kThreads), 0, st, bp, d_res, c->cfg.H, c->cfg.K, team,
              (const uint4*)yp, pos, topk_w, (const uint4*)residual, (uint4*)out);
   EB_LAUNCH_CHECK(c, "combine");
   return EB_OK;

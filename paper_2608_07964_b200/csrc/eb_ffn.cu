@@ -52,6 +52,7 @@
 #include <cstddef>
 #include <type_traits>
 
+#include "eb_mma.cuh"
 #include "eb_tiles.cuh"
 
 namespace {
@@ -75,154 +76,7 @@ constexpr int kParts = 4;                                      // tiles whose ep
                                                                // only when every reader has taken the one kItems before it, so at most kItems + 1
 static_assert(kParts > kItems, "a barrier of the publisher is free again before it comes round");
 constexpr int kAskAhead = 16;                                  // k-blocks before the end of a tile at which its successor is asked for
-constexpr long long kSpinLimitCycles = 4000000000LL;
 
-// ---- PTX wrappers ----------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// whether the phase is over, without waiting
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded waits: false if the limit expired or another thread of the CTA already gave up.
-template <typename Try>
-__device__ __forceinline__ bool bounded_wait(Try try_once, volatile int* s_abort, int* status, long long limit = kSpinLimitCycles) {
-  if (try_once()) return true;
-  const long long t0 = clock64();
-  for (uint32_t spin = 1;; ++spin) {
-    if (try_once()) return true;
-    if ((spin & 63u) == 0u) {
-      if (*s_abort) return false;
-      if (clock64() - t0 > limit) {
-        *s_abort = 1;
-        atomicExch(status, (int)EB_ERR_TIMEOUT);
-        return false;
-      }
-    }
-  }
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* s_abort, int* status,
-                                          long long limit = kSpinLimitCycles) {
-  return bounded_wait([&] { return mbar_try(bar, parity); }, s_abort, status, limit);
-}
-// the same for a barrier that the peer CTA's ordinary stores arrive with
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* s_abort, int* status) {
-  return bounded_wait([&] { return mbar_try_cluster(bar, parity); }, s_abort, status);
-}
-
-__device__ __forceinline__ void prefetch_tmap(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
-
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-// shared::cluster address of the same offset in CTA `rank` of the cluster
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Says "done with it" to a barrier of the pair: nothing this thread wrote is handed over.
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-// Hands what the warp wrote to a thread of the same CTA.
-__device__ __forceinline__ void mbar_arrive_release(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// The same as mbar_arrive_cluster with what this thread wrote before it.  Only the tile dealer uses it: a release at cluster scope waits for
-// the thread's earlier accesses, and in the producer, MMA and epilogue warps that cost 1 to 2 us per tile.
-__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-__device__ __forceinline__ void st_cluster(uint32_t cluster_addr, const int4& v) {
-  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ int4 ld_shared(uint32_t addr) {
-  int4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ int ld_acquire(const int* p) {
-  int v;
-  asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-  return v;
-}
-// Counts one up; what the thread has seen written goes before (release: a fence and a relaxed addition).  Between the two, what it has
-// seen is also put before later accesses of TMA units.  A step of 4 x 64 tokens, where every down tile waits for this, 33.5 -> 33.2 us
-// against a __threadfence and a red.release.
-__device__ __forceinline__ void red_publish(int* p) {
-  asm volatile("fence.acq_rel.gpu;" ::: "memory");
-  asm volatile("fence.proxy.async;" ::: "memory");
-  asm volatile("red.relaxed.gpu.global.add.s32 [%0], 1;" ::"l"(p) : "memory");
-}
-// orders ordinary memory accesses with those of the TMA unit
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
-// TMA loads whose completion is counted on a barrier that may live in the peer CTA (the data goes to the
-// issuing CTA only)
-__device__ __forceinline__ void tma_pair_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void tma_pair_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_alloc_pair(uint32_t dst_smem, uint32_t cols) {
-  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
-}
-__device__ __forceinline__ void tmem_relinquish_pair() {
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc_pair(uint32_t addr, uint32_t cols) {
-  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
-}
 // D[tmem of both CTAs] (+)= A * B^T with M = 256 (128 rows of A per CTA), N from the descriptor (half of B per CTA), K = 16
 __device__ __forceinline__ void umma_pair_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -231,38 +85,6 @@ __device__ __forceinline__ void umma_pair_bf16(uint32_t d_tmem, uint64_t a_desc,
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
       : "memory");
-}
-// arrives on the barrier at this offset in both CTAs of the pair once the MMAs issued so far are done
-__device__ __forceinline__ void umma_pair_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-               ::"r"(bar), "h"((uint16_t)3)
-               : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr)
-               : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// Shared-memory operand descriptor: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 // Instruction descriptor: fp32 accumulate, bf16 A and B, both K-major; M weight rows and N token columns.
 __device__ __forceinline__ uint32_t instr_desc(int m, int n) {
@@ -303,20 +125,6 @@ struct TmemTurn {
   __device__ __forceinline__ uint32_t col0() const { return (used & 3u) == 2u ? kTmemHalf : 0; }
   __device__ __forceinline__ uint32_t step() const { return (used & 3u) == 3u ? kTmemHalf : kNarrowCols; }
 };
-
-// An epilogue warp whose TMEM reads are complete (wait::ld) hands its part of an accumulator back to the MMA warp.
-__device__ __forceinline__ void release_tmem(uint32_t bar, int lane) {
-  tc_fence_before();
-  __syncwarp();
-  if (lane == 0) mbar_arrive_cluster(map_to_cta(bar, 0));
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ bf16 low_half(uint32_t v) { return __ushort_as_bfloat16((unsigned short)(v & 0xffffu)); }
-__device__ __forceinline__ bf16 high_half(uint32_t v) { return __ushort_as_bfloat16((unsigned short)(v >> 16)); }
 
 // Chunks at columns 0, kChunkStep, .. of an accumulator, rounded to bf16, two tokens per word.
 template <int N>
@@ -870,11 +678,11 @@ plan_kernel(ModelParams mp, const int32_t* __restrict__ group_off, const int32_t
     int head, n_slots;
     if (merged_class(mp, s_dev_off, nl, device, i, group_off, &head, &n_slots)) {
       // the class's tiles sit at its first position
-      const int tiles = i == head ? (n_slots + kMergeSlots - 1) / kMergeSlots : 0;
-      return Position{g, n_slots, tiles, cost_class(tiles, merged_cols(min(n_slots, kMergeSlots)))};
+      const int most = merge_slots(out.shift), tiles = i == head ? (n_slots + most - 1) / most : 0;
+      return Position{g, n_slots, tiles, cost_class(tiles, merged_cols(min(n_slots, most)))};
     }
-    const int rows = group_off[g + 1] - group_off[g], tiles = group_tiles(rows);
-    return Position{g, -1, tiles, cost_class(tiles, group_cols(rows))};
+    const int rows = group_off[g + 1] - group_off[g], tiles = group_tiles(rows, out.shift);
+    return Position{g, -1, tiles, cost_class(tiles, group_cols(rows, out.shift))};
   };
   order_tiles(g1 - g0, nl, device, g0, item, out, sh);
 }
@@ -887,37 +695,6 @@ fill_kernel(ModelParams mp, const int32_t* __restrict__ group_off, const int32_t
 }
 
 // ---- host side ---------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static const EncodeTiledFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return (EncodeTiledFn)p;
-  }();
-  return fn;
-}
-
-// bf16 tensor [d2][d1][d0] (d0 innermost), box {b0, b1, 1}, 128-byte swizzle, zero fill out of bounds
-bool make_map(CUtensorMap* m, const void* ptr, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t b0, uint32_t b1) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[3] = {d0, d1, d2};
-  cuuint64_t strides[2] = {d0 * 2, d0 * d1 * 2};
-  cuuint32_t box[3] = {b0, b1, 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  int rank = d2 > 0 ? 3 : 2;
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS;
-}
-
 cudaError_t launch_ffn(eb_ctx* c, cudaStream_t st, const FfnParams& p) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c->pair_grid);
@@ -945,6 +722,38 @@ eb_status ebi_selftest_wait(eb_ctx* c, cudaStream_t st, long long limit_cycles, 
   return EB_OK;
 }
 
+// How many CTAs of 2-CTA clusters of this kernel the device can hold at once (one CTA per SM); 0: none.
+int ebi_pair_grid(eb_ctx* c, const void* kernel, int threads, size_t smem) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (c->num_sms / 2));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess || clusters < 1) {
+    cudaGetLastError();
+    return 0;
+  }
+  return 2 * (clusters < c->num_sms / 2 ? clusters : c->num_sms / 2);
+}
+
+eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, bool fp8) {
+  {
+    KernelTimer timer(c, EBK_FFN_PLAN, st);
+    EB_LAUNCH(c, "expert_ffn", ebi_launch(plan_kernel, dim3(1), dim3(1024), 0, st, c->mp, group_off, step_meta, (int)device, tile_plan_of(c, fp8)));
+  }
+  KernelTimer timer(c, EBK_FFN_FILL, st);
+  EB_LAUNCH(c, "expert_ffn", ebi_launch(fill_kernel, dim3(c->num_sms), dim3(256), sizeof(int) * (size_t)(ebi_groups_cap(c) + 1), st, c->mp,
+                                        group_off, group_w, tile_list_of(c, fp8)));
+  return EB_OK;
+}
+
 eb_status ebi_ffn_bind(eb_ctx* c) {
   if (eb_status ds = ebi_check_device(c)) return ds;
   const eb_config& g = c->cfg;
@@ -957,25 +766,8 @@ eb_status ebi_ffn_bind(eb_ctx* c) {
   // per context: function attributes and cluster occupancy belong to the current device
   cudaError_t e = cudaFuncSetAttribute(ffn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return ebi_check_cuda(c, e, "cudaFuncSetAttribute");
-  // how many 2-CTA clusters of this kernel the device can hold at once (one CTA per SM)
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * (c->num_sms / 2));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  int clusters = 0;
-  e = cudaOccupancyMaxActiveClusters(&clusters, ffn_kernel, &cfg);
-  if (e != cudaSuccess || clusters < 1) {
-    cudaGetLastError();
-    return ebi_fail(c, EB_ERR_CUDA, "the device cannot hold a 2-CTA cluster of the expert kernel");
-  }
-  c->pair_grid = 2 * (clusters < c->num_sms / 2 ? clusters : c->num_sms / 2);
+  c->pair_grid = ebi_pair_grid(c, (const void*)ffn_kernel, kThreads, kSmemBytes);
+  if (!c->pair_grid) return ebi_fail(c, EB_ERR_CUDA, "the device cannot hold a 2-CTA cluster of the expert kernel");
   return EB_OK;
 }
 
@@ -1009,15 +801,8 @@ eb_status ebi_ffn_run(eb_ctx* c, cudaStream_t st, const void* xp, const int32_t*
   p.H = g.H;
   p.I = g.I;
   p.status = c->d_status;
-  if (!planned) {
-    {
-      KernelTimer timer(c, EBK_FFN_PLAN, st);
-      EB_LAUNCH(c, "expert_ffn", ebi_launch(plan_kernel, dim3(1), dim3(1024), 0, st, c->mp, group_off, step_meta, (int)device, tile_plan_of(c)));
-    }
-    KernelTimer timer(c, EBK_FFN_FILL, st);
-    EB_LAUNCH(c, "expert_ffn", ebi_launch(fill_kernel, dim3(c->num_sms), dim3(256), sizeof(int) * (size_t)(ebi_groups_cap(c) + 1), st, c->mp,
-                                          group_off, group_w, tile_list_of(c)));
-  }
+  if (!planned)
+    if (eb_status s = ebi_ffn_plan(c, st, group_off, group_w, step_meta, device, false)) return s;
   if (!c->timing) {
     p.part = 0;
     EB_LAUNCH(c, "expert_ffn", launch_ffn(c, st, p));

@@ -12,17 +12,21 @@
 // need the whole GPU to be through: the counts of all tokens, then the positions of all rows.  The counts travel as
 // chunk histograms, which also spares the routing its global atomics.
 #include <algorithm>
+#include <type_traits>
 
 #include "eb_dispatch.cuh"
+#include "eb_quant.cuh"
 #include "eb_route.cuh"
+#include "eb_scores.cuh"
 #include "eb_schedule.cuh"
 #include "eb_tiles.cuh"
 
 namespace {
 
-template <int PL>
-__global__ void __launch_bounds__(kChunkThreads, PL <= 2 ? 2 : 1)
-front_kernel(ModelParams mp, BatchParams bp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
+// kScored: by scores, groups and a bias (eb_scores.cuh)
+template <int PL, bool kScored>
+__global__ void __launch_bounds__(kChunkThreads, PL <= 2 && !kScored ? 2 : 1)
+front_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
              int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ chunk_hist) {
   __shared__ int s_hist[EB_MAX_E];
   const int c = blockIdx.x, j = mb_of_chunk(bp, c);
@@ -35,7 +39,10 @@ front_kernel(ModelParams mp, BatchParams bp, uint32_t pool_mask, uint32_t route_
   }
   EB_GRID_DEP_SYNC();
   if (!counted) return;
-  route_chunk<PL>(mp, bp, c, j, routed, logits, topk_idx, topk_w, s_hist);
+  route_chunk(mp, bp, c, j, routed, topk_idx, s_hist, [&](int t) {
+    if constexpr (kScored) return route_scored<PL>(mp, rp, t, bp.layer[j], lane, logits + (size_t)t * mp.E, topk_idx, topk_w);
+    else return route_token<PL>(mp, t, lane, logits, topk_idx, topk_w);
+  });
   for (int e = threadIdx.x; e < mp.E; e += kChunkThreads) chunk_hist[(size_t)c * mp.E + e] = s_hist[e];
 }
 
@@ -231,8 +238,8 @@ tables_kernel(const __grid_constant__ ModelParams mp, const __grid_constant__ Ba
     const int g = nl * (off + d * S) + lr * (n_d + S) + (k - off);
     s_goff[g] = tot;
     a.group_w[g] = s_act[lr] * (E + S) + e;
-    const int pos = nl * off + lr * n_d + (k - off), tiles = group_tiles(tot);
-    s_ptiles[pos] = tiles << 4 | (cost_class(tiles, group_cols(tot)) & 15);
+    const int pos = nl * off + lr * n_d + (k - off), tiles = group_tiles(tot, a.plan.shift);
+    s_ptiles[pos] = tiles << 4 | (cost_class(tiles, group_cols(tot, a.plan.shift)) & 15);
     a.plan.pgroup[pos] = g;
     a.plan.pslots[pos] = -1;
   }
@@ -260,8 +267,9 @@ tables_kernel(const __grid_constant__ ModelParams mp, const __grid_constant__ Ba
     s_goff[g] = rows;
     a.group_w[g] = s_act[lr] * (E + S) + E + s;
     const bool merged = D >= 2 && most <= kMergeMaxRows;
-    const int tiles = !merged ? group_tiles(rows) : d == 0 ? (n_slots + kMergeSlots - 1) / kMergeSlots : 0;
-    const int cols = merged ? merged_cols(min(n_slots, kMergeSlots)) : group_cols(rows);
+    const int slots = merge_slots(a.plan.shift);   // of a merged tile at most
+    const int tiles = !merged ? group_tiles(rows, a.plan.shift) : d == 0 ? (n_slots + slots - 1) / slots : 0;
+    const int cols = merged ? merged_cols(min(n_slots, slots)) : group_cols(rows, a.plan.shift);
     s_ptiles[pos] = tiles << 4 | (cost_class(tiles, cols) & 15);
     a.plan.pgroup[pos] = g;
     a.plan.pslots[pos] = merged ? n_slots : -1;
@@ -340,7 +348,9 @@ struct ScatterArgs {
   Segments seg;
   int32_t *pos, *row_src, *step_meta;
   const uint4* x;
-  uint4* xp;
+  uint4* xp;             // the rows as they are, or
+  uint2* xq;             // as e4m3 values with their scales [rows][ceil(H / 128)] (8-bit weights)
+  float* xs;
   TileList list;
   int fill_blocks;
   int team;   // threads per token row
@@ -358,7 +368,10 @@ struct ScatterArgs {
 // time and TB = 8, 84 with teams and 29 with the whole chunk (44 for separate rank, gather and fill kernels), 16 x 2048 of 512
 // elements 64 with teams and 46.  Wide rows need the blocks: with 2048 elements, 16 x 512 tokens take 45 us at TB = 8 and 74 at
 // 32, with 1000 and 16 x 2048 both take 90.
-template <int TB>
+//
+// kQuant: the rows go out as e4m3 values.  The sixteen threads that hold a block of 128 elements find its scale by four shuffles, so a row is
+// still read once, and quantised once for its K + S places, which take half the bytes.
+template <int TB, bool kQuant>
 __global__ void __launch_bounds__(kScatterThreads)
 scatter_kernel(const __grid_constant__ ModelParams mp, const __grid_constant__ BatchParams bp, const __grid_constant__ ScatterArgs a) {
   extern __shared__ int s_dyn[];
@@ -477,26 +490,51 @@ scatter_kernel(const __grid_constant__ ModelParams mp, const __grid_constant__ B
     }
   }
   __syncthreads();
+  const int blocks = ebi_blocks(mp.H);
   auto move_rows = [&](int row0, bool loaded) {
-    for (int col = col0; col < vec; col += a.team) {
+    // quantising, the warp stays together for its shuffles
+    for (int col = col0; kQuant ? col - col0 < vec : col < vec; col += a.team) {
       if (!loaded) {
 #pragma unroll
         for (int k = 0; k < P; ++k)
-          if (row0 + k * teams < nt) v[k] = __ldg(a.x + (size_t)(t0 + row0 + k * teams) * vec + col);
+          if (row0 + k * teams < nt && (!kQuant || col < vec)) v[k] = __ldg(a.x + (size_t)(t0 + row0 + k * teams) * vec + col);
       }
       loaded = false;
+      if constexpr (kQuant) {
 #pragma unroll
-      for (int k = 0; k < P; ++k)
-        if (row0 + k * teams < nt)
-          for (int s = 0; s < KS; ++s) {
-            const int p = s_pos[row0 + k * teams][s];
-            if (p >= 0) a.xp[(size_t)p * vec + col] = v[k];
-          }
+        for (int k = 0; k < P; ++k) {
+          const bool there = row0 + k * teams < nt && col < vec;
+          if (!__any_sync(0xffffffffu, there)) continue;
+          if (!there) v[k] = make_uint4(0, 0, 0, 0);
+          const BlockScale sc = warp_block_scale(v[k], a.team);
+          const uint2 q = quantise8(sc, v[k]);
+          if (there)
+            for (int s = 0; s < KS; ++s) {
+              const int p = s_pos[row0 + k * teams][s];
+              if (p < 0) continue;
+              a.xq[(size_t)p * vec + col] = q;
+              if ((col & 15) == 0) a.xs[(size_t)p * blocks + (col >> 4)] = sc.scale;
+            }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+          if (row0 + k * teams < nt)
+            for (int s = 0; s < KS; ++s) {
+              const int p = s_pos[row0 + k * teams][s];
+              if (p >= 0) a.xp[(size_t)p * vec + col] = v[k];
+            }
+      }
     }
   };
   move_rows(team, true);
-  if constexpr (TB > P)
-    for (int row0 = team + P * teams; row0 < nt; row0 += P * teams) move_rows(row0, false);
+  if constexpr (TB > P) {
+    if constexpr (kQuant) {   // as many rounds for every team, for the shuffles
+      for (int r = P * teams; r < nt; r += P * teams) move_rows(team + r, false);
+    } else {
+      for (int row0 = team + P * teams; row0 < nt; row0 += P * teams) move_rows(row0, false);
+    }
+  }
 }
 
 // tables_kernel adds the chunk histograms up itself below this many words (chunks times experts) and up to this many chunks
@@ -563,7 +601,9 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
   }
   if (bp.n_chunks > 0) {
     KernelTimer timer(c, EBK_ROUTE, st);
-    EB_LAUNCH(c, "front", ebi_launch(g.E <= 64 ? front_kernel<2> : front_kernel<kMaxPerLane>, dim3(bp.n_chunks), dim3(kChunkThreads), 0, st, c->mp, bp,
+    auto kernel = c->scored ? (g.E <= 64 ? front_kernel<2, true> : front_kernel<kMaxPerLane, true>)
+                            : (g.E <= 64 ? front_kernel<2, false> : front_kernel<kMaxPerLane, false>);
+    EB_LAUNCH(c, "front", ebi_launch(kernel, dim3(bp.n_chunks), dim3(kChunkThreads), 0, st, c->mp, bp, c->router,
                                      pool_mask, route_mask, (const float*)b->logits, b->topk_idx, b->topk_w, c->chunk_hist));
   }
   Segments seg;
@@ -578,7 +618,7 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
       EB_LAUNCH(c, "sums", ebi_launch(sums_kernel, dim3((seg.off[EB_MAX_MB] * g.E + 255) / 256), dim3(256), 0, st, c->mp, bp, seg, pool_mask | route_mask,
                                       (const int32_t*)c->chunk_hist, c->chunk_base, c->chunk_seg));
     const TablesArgs a{pool_mask, route_mask, (int)m, (int)policy, c->chunk_hist, sums ? c->chunk_seg : nullptr, c->chunk_base, c->seg_base,
-                       c->mb_base, b->mb_load, b->mb_cnt, seg, layers_of(bp), b->sched, b->group_off, b->group_w, b->step_meta, tile_plan_of(c),
+                       c->mb_base, b->mb_load, b->mb_cnt, seg, layers_of(bp), b->sched, b->group_off, b->group_w, b->step_meta, tile_plan_of(c, c->use_fp8),
                        sched_grid_of(c)};
     int blocks = sched_blocks(pool_mask, m, policy);
     if ((int64_t)sched_subsets(pool_mask, m) * (blocks - 1) / blocks < kSchedSubsets) blocks = 1;
@@ -595,16 +635,20 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
     const int members = __builtin_popcount(pool_mask), sure = policy == EB_POLICY_ALL ? members : std::min((int)m, members);
     const uint32_t touch_mask = 2 * sure >= members ? pool_mask : 0;
     const ScatterArgs a{b->sched, b->topk_idx, c->chunk_base, sums ? c->seg_base : nullptr, c->mb_base, b->group_off, b->group_w, seg, b->pos, b->row_src, b->step_meta,
-                        (const uint4*)b->x, (uint4*)b->xp, tile_list_of(c), c->num_sms / 2, row_team(g.H / 8), touch_mask,
+                        (const uint4*)b->x, (uint4*)b->xp, (uint2*)b->xp, ebi_row_scales(c, b->xp), tile_list_of(c, c->use_fp8), c->num_sms / 2, row_team(g.H / 8), touch_mask,
                         b->mb_load, schedule_watch_of(c)};
     const size_t smem = sizeof(int) * (size_t)(ebi_groups_cap(c) + 1);
     auto launch = [&](auto kernel, int tb) {
       return ebi_launch(kernel, dim3((a.watch.rec ? 1 : 0) + a.fill_blocks + bp.n_chunks * (32 / tb)), dim3(kScatterThreads), smem, st, c->mp, bp, a);
     };
-    EB_LAUNCH(c, "scatter", bp.n_tok <= 2 * c->num_sms     ? launch(scatter_kernel<1>, 1)
-                            : bp.n_tok <= 16 * c->num_sms  ? launch(scatter_kernel<4>, 4)
-                            : g.H > kScatterNarrow || bp.n_tok <= 64 * c->num_sms ? launch(scatter_kernel<8>, 8)
-                                                                                  : launch(scatter_kernel<32>, 32));
+    auto scatter = [&](auto quant) {
+      constexpr bool kQuant = decltype(quant)::value;
+      return bp.n_tok <= 2 * c->num_sms     ? launch(scatter_kernel<1, kQuant>, 1)
+             : bp.n_tok <= 16 * c->num_sms  ? launch(scatter_kernel<4, kQuant>, 4)
+             : g.H > kScatterNarrow || bp.n_tok <= 64 * c->num_sms ? launch(scatter_kernel<8, kQuant>, 8)
+                                                                   : launch(scatter_kernel<32, kQuant>, 32);
+    };
+    EB_LAUNCH(c, "scatter", c->use_fp8 ? scatter(std::true_type()) : scatter(std::false_type()));
   }
   ebi_watch_launched(c, st);
   EB_LAUNCH_CHECK(c, "step front end");

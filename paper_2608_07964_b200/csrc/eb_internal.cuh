@@ -56,6 +56,14 @@ struct ModelParams {
   const int32_t* e_local;   // [E] index of the expert among its device's experts
 };
 
+// Gating by scores, groups and a balance bias (eb_router), as kernels take it.
+struct RouterParams {
+  int32_t sigmoid;                          // 1: sigmoid scores, 0: softmax
+  int32_t n_group, topk_group, group_top;
+  float scale;
+  const float* bias;                        // [L][E] or null
+};
+
 // Record of a schedule in pinned host memory (eb_watch_schedule).
 struct ScheduleRecord {
   eb_sched_result res;
@@ -86,6 +94,17 @@ struct eb_ctx {
   const bf16* w_up = nullptr;
   const bf16* w_down = nullptr;
   CUtensorMap tm_gate, tm_up, tm_down, tm_gate64, tm_up64;
+  // 8-bit expert path (eb_enable_fp8): e4m3 weights with a scale per 128 x 128 block
+  bool fp8 = false;                // the workspace is laid out for it too
+  bool use_fp8 = false;            // the weights bound last are 8-bit ones
+  const void *w8_gate = nullptr, *w8_up = nullptr, *w8_down = nullptr;
+  const float *s8_gate = nullptr, *s8_up = nullptr, *s8_down = nullptr;
+  CUtensorMap tm8_gate, tm8_up, tm8_down;
+  int pair_grid8 = 0;              // as pair_grid, of the 8-bit expert kernel
+  float* act_scale = nullptr;      // [ceil(I / 128)][R_cap] scales of the 8-bit intermediate, which lies in `act`
+  RouterParams router = {};        // of eb_set_router
+  bool scored = false;             // eb_route and whole steps route by it
+
   int pair_grid = 0;               // CTAs launched for the expert kernels: two per 2-CTA cluster the device holds at once
 
   // workspace carve-up
@@ -211,6 +230,11 @@ static inline cudaError_t ebi_launch(void (*kernel)(KArgs...), dim3 grid, dim3 b
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Blocks of 128 elements in a row: the columns of its scales.
+static inline __host__ __device__ int ebi_blocks(int n) { return (n + 127) / 128; }
+// The scales that follow the e4m3 rows in eb_step_buffers.xp.
+static inline float* ebi_row_scales(const eb_ctx* c, void* xp) { return (float*)((char*)xp + (size_t)ebi_rows_cap(c) * c->cfg.H); }
+
 static inline bool ebi_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Entry points of the per-step stages (defined in their own translation units).
@@ -220,4 +244,12 @@ eb_status ebi_ffn_run(eb_ctx* c, cudaStream_t st, const void* xp, const int32_t*
 eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint32_t pool_mask, uint32_t route_mask, int32_t m,
                         eb_policy policy, const eb_step_buffers* b);
 eb_status ebi_ffn_bind(eb_ctx* c);
+// The same for 8-bit weights (eb_ffn8.cu); the tile list of an expert pass that is not planned (eb_ffn.cu).
+eb_status ebi_ffn8_bind(eb_ctx* c);
+eb_status ebi_ffn8_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
+                       const int32_t* step_meta, void* yp, int32_t device, bool planned = false);
+eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, bool fp8);
+int ebi_pair_grid(eb_ctx* c, const void* kernel, int threads, size_t smem);
+// The host checks of a router; false: why not in *why.
+bool ebi_router_ok(const eb_config& g, const eb_router* r, RouterParams* out, const char** why);
 eb_status ebi_selftest_wait(eb_ctx* c, cudaStream_t st, long long limit_cycles, int* d_gave_up);

@@ -13,6 +13,7 @@
 #include <cstring>
 
 #include "eb_dispatch.cuh"
+#include "eb_quant.cuh"
 
 namespace {
 
@@ -446,7 +447,7 @@ gather_kernel(int n_tok, int H, int KS, int team, const uint4* __restrict__ x, c
   if (t >= n_tok) return;
   const int lane = threadIdx.x & 31;
   const int my_pos = lane < KS ? pos[(size_t)t * KS + lane] : -1;   // lane s fetches slot s once per warp
-  if (__shfl_sync(0xffffffffu, my_pos, 0) < 0) return;              // micro-batch does not run
+  if (!__any_sync(0xffffffffu, my_pos >= 0)) return;                // micro-batch does not run
   const int vec = H / 8;  // 16-byte vectors per row
   const uint4* src = x + (size_t)t * vec;
   for (int v0 = 0; v0 < vec; v0 += team) {
@@ -460,20 +461,49 @@ gather_kernel(int n_tok, int H, int KS, int team, const uint4* __restrict__ x, c
   }
 }
 
+// The same with the rows as e4m3 values and a scale for each block of 128 elements: the row is read and quantised once.
+__global__ void __launch_bounds__(kGatherThreads)
+gather_quant_kernel(int n_tok, int H, int KS, int team, const uint4* __restrict__ x, const int32_t* __restrict__ pos,
+                    uint2* __restrict__ xq, float* __restrict__ xs) {
+  EB_GRID_DEP_SYNC();
+  const int t = blockIdx.x * (kGatherThreads / team) + threadIdx.x / team;
+  if (t >= n_tok) return;
+  const int lane = threadIdx.x & 31;
+  const int my_pos = lane < KS ? pos[(size_t)t * KS + lane] : -1;
+  if (!__any_sync(0xffffffffu, my_pos >= 0)) return;
+  const int vec = H / 8, blocks = ebi_blocks(H);
+  const uint4* src = x + (size_t)t * vec;
+  for (int v0 = 0; v0 < vec; v0 += team) {
+    const int v = v0 + threadIdx.x % team;
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (v < vec) r = __ldg(src + v);
+    const BlockScale sc = warp_block_scale(r, team);
+    const uint2 q = quantise8(sc, r);
+    for (int s = 0; s < KS; ++s) {
+      const int p = __shfl_sync(0xffffffffu, my_pos, s);
+      if (v < vec && p >= 0) {
+        xq[(size_t)p * vec + v] = q;
+        if ((v & 15) == 0) xs[(size_t)p * blocks + (v >> 4)] = sc.scale;
+      }
+    }
+  }
+}
+
 static inline int team_for(int vec) { return vec <= 32 ? 32 : vec <= 64 ? 64 : vec <= 128 ? 128 : 256; }
 
 }  // namespace
 
-extern "C" eb_status eb_permute(eb_ctx* c, void* stream, const eb_batch* batch, const eb_sched_result* d_res,
-                                const void* x, const int32_t* topk_idx, int32_t* group_off, int32_t* group_w,
-                                int32_t* row_src, int32_t* pos, void* xp, int32_t* step_meta) {
-  if (!c) return EB_ERR_INVALID_ARG;
+// The dispatch of eb_permute; xs: scales of quantised rows, null for rows as they are.
+static eb_status permute_run(eb_ctx* c, void* stream, const eb_batch* batch, const eb_sched_result* d_res, const void* x,
+                             const int32_t* topk_idx, int32_t* group_off, int32_t* group_w, int32_t* row_src, int32_t* pos, void* xp,
+                             bool quant, float* xs, int32_t* step_meta) {
   BatchParams bp;
   eb_status s = ebi_make_batch(c, batch, &bp);
   if (s != EB_OK) return s;
-  if (!d_res || !x || !topk_idx || !group_off || !group_w || !row_src || !pos || !xp || !step_meta)
+  if (!d_res || !x || !topk_idx || !group_off || !group_w || !row_src || !pos || !xp || !step_meta || (quant && !xs))
     return ebi_fail(c, EB_ERR_INVALID_ARG, "null pointer");
   if (!ebi_aligned16(x) || !ebi_aligned16(xp)) return ebi_fail(c, EB_ERR_INVALID_ARG, "x / xp must be 16-byte aligned");
+  if (!ebi_aligned16(xs)) return ebi_fail(c, EB_ERR_INVALID_ARG, "xs must be 16-byte aligned");
   if (!c->ws) return ebi_fail(c, EB_ERR_WORKSPACE, "no workspace set");
   cudaStream_t st = (cudaStream_t)stream;
   const int gcap = ebi_groups_cap(c);
@@ -513,11 +543,30 @@ extern "C" eb_status eb_permute(eb_ctx* c, void* stream, const eb_batch* batch, 
   if (bp.n_tok > 0) {
     KernelTimer timer(c, EBK_PERMUTE_GATHER, st);
     const int team = team_for(c->cfg.H / 8), tpb = kGatherThreads / team;
-    EB_LAUNCH(c, "permute", ebi_launch(gather_kernel, dim3((bp.n_tok + tpb - 1) / tpb), dim3(kGatherThreads), 0, st, bp.n_tok, c->cfg.H,
-                                       c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint4*)xp));
+    if (quant)
+      EB_LAUNCH(c, "permute", ebi_launch(gather_quant_kernel, dim3((bp.n_tok + tpb - 1) / tpb), dim3(kGatherThreads), 0, st, bp.n_tok, c->cfg.H,
+                                         c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint2*)xp, xs));
+    else
+      EB_LAUNCH(c, "permute", ebi_launch(gather_kernel, dim3((bp.n_tok + tpb - 1) / tpb), dim3(kGatherThreads), 0, st, bp.n_tok, c->cfg.H,
+                                         c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint4*)xp));
   }
   EB_LAUNCH_CHECK(c, "permute");
   return EB_OK;
+}
+
+extern "C" eb_status eb_permute(eb_ctx* c, void* stream, const eb_batch* batch, const eb_sched_result* d_res,
+                                const void* x, const int32_t* topk_idx, int32_t* group_off, int32_t* group_w,
+                                int32_t* row_src, int32_t* pos, void* xp, int32_t* step_meta) {
+  if (!c) return EB_ERR_INVALID_ARG;
+  return permute_run(c, stream, batch, d_res, x, topk_idx, group_off, group_w, row_src, pos, xp, false, nullptr, step_meta);
+}
+
+extern "C" eb_status eb_permute_fp8(eb_ctx* c, void* stream, const eb_batch* batch, const eb_sched_result* d_res, const void* x,
+                                    const int32_t* topk_idx, int32_t* group_off, int32_t* group_w, int32_t* row_src, int32_t* pos,
+                                    void* xq, float* xs, int32_t* step_meta) {
+  if (!c) return EB_ERR_INVALID_ARG;
+  if (!c->fp8) return ebi_fail(c, EB_ERR_INVALID_ARG, "eb_enable_fp8 first");
+  return permute_run(c, stream, batch, d_res, x, topk_idx, group_off, group_w, row_src, pos, xq, true, xs, step_meta);
 }
 
 // ---- eb_check_permutation ----------------------------------------------------------------------
@@ -564,6 +613,7 @@ check_kernel(ModelParams mp, BatchParams bp, int rows_cap, int groups_cap, const
       if (p != -1) ++bad;
       continue;
     }
+    if (slot < mp.K && p == -1 && topk_idx[(size_t)t * mp.K + slot] == -1) continue;   // an empty slot
     if (p < 0 || p >= R) {
       ++bad;
       continue;

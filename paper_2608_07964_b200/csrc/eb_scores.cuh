@@ -1,0 +1,210 @@
+// Gating by scores, groups and a balance bias (eb_router), one token by one warp; lane i holds logits i, i+32, ...
+//
+//   s_e = sigmoid(z_e) or softmax(z)_e;   c_e = s_e + bias[layer][e], what the choice goes by
+//   value of a group = the best c_e of its experts, or the sum of the best two; the topk_group best groups stay
+//   the K best c_e of these groups; w = scale * s_e, over the sum of the chosen s_e if renormalised
+//
+// Order is what has to be exact: two c_e that differ by less than a rounding of 32 bits change places otherwise, and with them a
+// token's experts.  Without a bias c_e orders like z_e, so the logits are compared (integers in the order of the floats); a
+// sum, of a bias or of two scores, is made and compared in 64 bits.
+#pragma once
+
+#include <cfloat>
+
+#include "eb_route.cuh"
+
+namespace {
+
+__device__ __forceinline__ float logit_value(float z) { return z; }
+__device__ __forceinline__ float logit_value(bf16 z) { return __bfloat162float(z); }
+
+// Unsigned integers in the order of the doubles; 0 stands for "no candidate".
+__device__ __forceinline__ unsigned long long double_key(double v) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
+  return (b >> 63) ? ~b : (b | (1ull << 63));
+}
+__device__ __forceinline__ double key_double(unsigned long long k) {
+  return __longlong_as_double((long long)((k >> 63) ? (k & ~(1ull << 63)) : ~k));
+}
+__device__ __forceinline__ unsigned warp_max(unsigned k) { return __reduce_max_sync(0xffffffffu, k); }
+__device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
+  const unsigned hi = __reduce_max_sync(0xffffffffu, (unsigned)(k >> 32));
+  const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
+  return ((unsigned long long)hi << 32) | lo;
+}
+// the sum of two values as keys; of the first alone where there is no second
+__device__ __forceinline__ unsigned key_sum(unsigned a, unsigned) { return a; }   // never asked for
+__device__ __forceinline__ unsigned long long key_sum(unsigned long long a, unsigned long long b) {
+  return b ? double_key(key_double(a) + key_double(b)) : a;
+}
+
+// Takes the best key of the warp: its value (0: none left) and, in *expert, the lowest index that has it; the holder's key is cleared.
+template <int PL, typename Key>
+__device__ __forceinline__ Key take_best(Key (&key)[PL], int lane, int* expert) {
+  Key best = key[0];
+  int at = 0;
+#pragma unroll
+  for (int i = 1; i < PL; ++i)
+    if (key[i] > best) {   // ascending i keeps the lower index on ties
+      best = key[i];
+      at = i;
+    }
+  const Key top = warp_max(best);
+  const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (unsigned)(lane + 32 * at) : 0xffffffffu);
+#pragma unroll
+  for (int i = 0; i < PL; ++i)
+    if (lane + 32 * i == e) key[i] = 0;
+  *expert = top ? e : -1;
+  return top;
+}
+
+// Clears the keys of the experts whose groups are not kept.
+template <int PL, typename Key>
+__device__ __forceinline__ void keep_groups(const RouterParams& rp, int E, int lane, Key (&key)[PL]) {
+  const int size = E / rp.n_group;
+  Key value = 0;   // lane g: of group g
+  for (int g = 0; g < rp.n_group; ++g) {
+    Key a = 0, b = 0;   // the lane's best two of the group
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      const int e = lane + 32 * i;
+      const Key k = e >= g * size && e < (g + 1) * size ? key[i] : 0;
+      if (k > a) {
+        b = a;
+        a = k;
+      } else if (k > b) {
+        b = k;
+      }
+    }
+    Key top = warp_max(a);
+    if (rp.group_top == 2) {
+      // the holder (one of them) offers its second best
+      const unsigned holders = __ballot_sync(0xffffffffu, a == top);
+      const Key second = warp_max(lane == __ffs(holders) - 1 ? b : a);
+      top = top ? key_sum(top, second) : 0;
+    }
+    if (lane == g) value = top;
+  }
+  unsigned kept = 0;
+  for (int n = 0; n < rp.topk_group; ++n) {
+    const Key top = warp_max(value);
+    if (!top) break;
+    const int g = __ffs(__ballot_sync(0xffffffffu, value == top)) - 1;
+    kept |= 1u << g;
+    if (lane == g) value = 0;
+  }
+#pragma unroll
+  for (int i = 0; i < PL; ++i)
+    if (!((kept >> min((lane + 32 * i) / size, 31)) & 1u)) key[i] = 0;
+}
+
+// The K best keys: expert number `lane` and its logit in lanes below K (-1: none left).
+template <int PL, typename Key>
+__device__ __forceinline__ int choose(int K, int lane, Key (&key)[PL], const float (&z)[PL], float* my_z) {
+  int my_e = -1;
+  float mine = 0.f;
+  for (int k = 0; k < K; ++k) {
+    int e;
+    if (!take_best<PL>(key, lane, &e)) break;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      if (lane + 32 * i == e) v = z[i];
+    v = __shfl_sync(0xffffffffu, v, e & 31);
+    if (lane == k) {
+      my_e = e;
+      mine = v;
+    }
+  }
+  *my_z = mine;
+  return my_e;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_largest(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// Routes token t (E <= 32 PL), whose logits are zs[0 .. E): writes its row of topk_idx and topk_w.  Returns expert number `lane` in lanes
+// below K.  A logit of -inf or NaN is an expert that cannot be chosen, one above the largest float counts as that.
+template <int PL, typename Z>
+__device__ __forceinline__ int route_scored(const ModelParams& mp, const RouterParams& rp, int t, int layer, int lane, const Z* __restrict__ zs,
+                                            int32_t* __restrict__ topk_idx, float* __restrict__ topk_w) {
+  const int E = mp.E, K = mp.K;
+  float z[PL];
+#pragma unroll
+  for (int i = 0; i < PL; ++i) {
+    const float v = lane + 32 * i < E ? logit_value(zs[lane + 32 * i]) : -INFINITY;
+    z[i] = v == v ? fminf(v, FLT_MAX) : -INFINITY;
+  }
+  float z_top = -INFINITY;
+  if (!rp.sigmoid) {
+#pragma unroll
+    for (int i = 0; i < PL; ++i) z_top = fmaxf(z_top, z[i]);
+    z_top = warp_largest(z_top);
+  }
+  int my_e;
+  float my_z;
+  if (!rp.bias && (rp.n_group == 1 || rp.group_top == 1)) {
+    unsigned key[PL];
+#pragma unroll
+    for (int i = 0; i < PL; ++i) key[i] = z[i] > -INFINITY ? float_key(z[i]) : 0u;
+    if (rp.n_group > 1) keep_groups<PL>(rp, E, lane, key);
+    my_e = choose<PL>(K, lane, key, z, &my_z);
+  } else {
+    double p[PL], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      if (rp.sigmoid) p[i] = 1.0 / (1.0 + exp(-(double)z[i]));
+      else p[i] = z[i] > -INFINITY ? exp((double)z[i] - (double)z_top) : 0.0;
+      sum += p[i];
+    }
+    if (!rp.sigmoid) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    unsigned long long key[PL];
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      const int e = lane + 32 * i;
+      const double s = rp.sigmoid ? p[i] : p[i] / sum;
+      const double c = s + (rp.bias && e < E ? (double)__ldg(rp.bias + (size_t)layer * E + e) : 0.0);
+      key[i] = z[i] > -INFINITY && c > -INFINITY ? double_key(c) : 0ull;
+    }
+    if (rp.n_group > 1) keep_groups<PL>(rp, E, lane, key);
+    my_e = choose<PL>(K, lane, key, z, &my_z);
+  }
+  // weights: the scores, over their sum with the power of e that the largest chosen one holds taken out, so that no sum vanishes
+  const bool there = lane < K && my_e >= 0;
+  float w;
+  if (rp.sigmoid) {
+    const float shift = mp.renorm ? fminf(warp_largest(there ? my_z : -INFINITY), 0.f) : 0.f;
+    w = my_z > 0.f ? 1.f / (1.f + expf(-my_z)) : expf(my_z - shift) / (1.f + expf(my_z));
+  } else {
+    const float shift = mp.renorm ? warp_largest(there ? my_z : -INFINITY) : z_top;
+    w = expf(my_z - shift);
+  }
+  if (!there) w = 0.f;
+  float total = 1.f;
+  if (mp.renorm) {
+    total = warp_sum(w);
+  } else if (!rp.sigmoid) {
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) total += z[i] > -INFINITY ? expf(z[i] - z_top) : 0.f;
+    total = warp_sum(total);
+  }
+  if (lane < K) {
+    topk_idx[(size_t)t * K + lane] = my_e;
+    topk_w[(size_t)t * K + lane] = there ? rp.scale * (w / total) : 0.f;
+  }
+  return my_e;
+}
+
+}  // namespace

@@ -6,10 +6,11 @@
 namespace {
 
 constexpr int kTileRows = 256;                                 // token rows of a tile at most
+constexpr int kTileShift = 8, kTileShift8 = 7;                 // as powers of two: bf16 tiles, 8-bit tiles (of 128 rows at most)
 constexpr int kFeat1 = 256;                                    // outputs of a gate/up tile
 constexpr int kFeat2 = 512;                                    // outputs of a down tile
 constexpr int kSlotRows = 16;                                  // rows of one slot of a merged tile
-constexpr int kMergeSlots = kTileRows / kSlotRows;             // slots of a merged tile at most
+constexpr int kMergeSlots = kTileRows / kSlotRows;             // slots of a merged tile at most (8-bit tiles: half of them)
 constexpr int kMergeMaxRows = 64;                              // replicas of a shared expert are merged when none has more rows
 
 // Accumulator columns of a tile of `valid_rows` token rows: rounded up to 16 (each CTA of the pair supplies half
@@ -36,12 +37,13 @@ struct Tile {
 };
 static_assert(sizeof(Tile) == 32, "two 16-byte words");
 
-// A group of `rows` rows is cut into ceil(rows / 256) tiles of nearly equal size, so no tile is a short
-// remainder that would still stream a whole weight tile.
-__device__ __forceinline__ int group_tiles(int rows) { return (rows + kTileRows - 1) / kTileRows; }
+// A group of `rows` rows is cut into ceil(rows / 256) tiles (8-bit: 128) of nearly equal size, so no tile is a short
+// remainder that would still stream a whole weight tile.  shift: kTileShift or kTileShift8.
+__device__ __forceinline__ int group_tiles(int rows, int shift) { return (rows + (1 << shift) - 1) >> shift; }
+__device__ __forceinline__ int merge_slots(int shift) { return (1 << shift) / kSlotRows; }
 // Columns (token rows rounded up to 16) of the largest tile of a group; its cost class is that count in steps of 32.
-__device__ __forceinline__ int group_cols(int rows) {
-  const int t = group_tiles(rows);
+__device__ __forceinline__ int group_cols(int rows, int shift) {
+  const int t = group_tiles(rows, shift);
   return t ? tile_cols((rows + t - 1) / t) : 0;
 }
 
@@ -97,6 +99,7 @@ struct TilePlan {
   int4* prank;
   int32_t *order, *tile_pref, *work_count;
   int nt1, nt2;   // output tiles of the two phases
+  int shift;      // rows of a tile at most, as a power of two
 };
 // One position of the processing order.
 struct Position {
@@ -229,7 +232,7 @@ __device__ __forceinline__ void order_tiles(int ng, int nl, int device, int g0, 
 // once per block, the binary search below then stays on chip.
 struct TileList {
   const int32_t *pgroup, *pslots, *order, *tile_pref, *work_count;
-  int nt1, nt2, max_work;
+  int nt1, nt2, shift, max_work;
   Tile* work;
   int32_t* ready;
   int2* slots;
@@ -263,9 +266,9 @@ __device__ __forceinline__ void fill_tiles(const ModelParams& mp, const int32_t*
     const int pos = order[lo], g = pgroup[pos], n_slots = pslots[pos];
     Tile it;
     if (n_slots >= 0) {
-      // tile m of a merged class holds the next 16 slots of the class, replicas in device order
-      const int base = kMergeSlots * (s_pref[lo] + m);
-      const int first = kMergeSlots * m, n_here = min(kMergeSlots, n_slots - first);
+      // tile m of a merged class holds the next 16 (8-bit: 8) slots of the class, replicas in device order
+      const int most = merge_slots(l.shift), base = kMergeSlots * (s_pref[lo] + m);
+      const int first = most * m, n_here = min(most, n_slots - first);
       if (list == 0 && n == 0) {
         int c = 0;   // slots before the current replica
         for (int d = 0; d < mp.D; ++d) {
@@ -300,14 +303,14 @@ __device__ __forceinline__ void fill_tiles(const ModelParams& mp, const int32_t*
   }
 }
 
-// The context's tile tables as the planning and filling blocks take them.
-inline TilePlan tile_plan_of(const eb_ctx* c) {
+// The context's tile tables as the planning and filling blocks take them, for the bf16 or the 8-bit expert pass.
+inline TilePlan tile_plan_of(const eb_ctx* c, bool fp8) {
   const int nt1 = (c->cfg.I + kFeat1 - 1) / kFeat1, nt2 = (c->cfg.H + kFeat2 - 1) / kFeat2;
-  return TilePlan{c->pgroup, c->pslots, c->prank, c->order, c->tile_pref, c->work_count, nt1, nt2};
+  return TilePlan{c->pgroup, c->pslots, c->prank, c->order, c->tile_pref, c->work_count, nt1, nt2, fp8 ? kTileShift8 : kTileShift};
 }
-inline TileList tile_list_of(const eb_ctx* c) {
-  const TilePlan p = tile_plan_of(c);
-  return TileList{c->pgroup, c->pslots, c->order, c->tile_pref, c->work_count, p.nt1, p.nt2, c->max_work, (Tile*)c->work, c->tile_ready, c->slots};
+inline TileList tile_list_of(const eb_ctx* c, bool fp8) {
+  const TilePlan p = tile_plan_of(c, fp8);
+  return TileList{c->pgroup, c->pslots, c->order, c->tile_pref, c->work_count, p.nt1, p.nt2, p.shift, c->max_work, (Tile*)c->work, c->tile_ready, c->slots};
 }
 
 }  // namespace
