@@ -86,8 +86,9 @@ static size_t carve(eb_ctx* c, char* base) {
   };
   c->max_chunks = (g.max_tokens + 31) / 32 + EB_MAX_MB;
   int rows = ebi_rows_cap(c), gcap = ebi_groups_cap(c);
-  c->max_tiles = rows / (c->fp8 ? 128 : 256) + gcap;   // a group of r rows has ceil(r / 256) tiles, ceil(r / 128) with 8-bit weights
-  c->max_work = c->max_tiles * ((g.I + 255) / 256 + (g.H + 511) / 512);   // 256 outputs per gate/up tile, 512 per down tile
+  c->max_tiles = rows / (c->fp8 && !c->fp8_many ? 128 : 256) + gcap;   // a group of r rows has ceil(r / 256) tiles, ceil(r / 128) with 8-bit weights for few rows
+  // 256 outputs per gate/up tile, 512 per down tile; half of that with 8-bit weights for many rows
+  c->max_work = c->max_tiles * (c->fp8_many ? (g.I + 127) / 128 + (g.H + 255) / 256 : (g.I + 255) / 256 + (g.H + 511) / 512);
   c->chunk_hist = (int32_t*)take(sizeof(int32_t) * (size_t)c->max_chunks * g.E);
   c->chunk_base = (int32_t*)take(sizeof(int32_t) * (size_t)c->max_chunks * g.E);
   c->chunk_seg = (int32_t*)take(sizeof(int32_t) * (size_t)(c->max_chunks / EB_SEG_CHUNKS + EB_MAX_MB) * g.E);
@@ -211,6 +212,9 @@ extern "C" eb_status eb_enable_fp8(eb_ctx* c) {
   if (c->cfg.H % 16 || c->cfg.I % 16) return ebi_fail(c, EB_ERR_UNSUPPORTED, "8-bit weights need H % 16 == 0 and I % 16 == 0");
   if (c->fp8) return EB_OK;
   c->fp8 = true;
+  // Two kernels (eb_ffn8_few.cu, eb_ffn8_many.cu).  Which rows an expert gets is not known before the routing, so the context's capacity decides:
+  // whether the largest batch, all of it at one layer, gives an expert more than 64 rows on average.
+  c->fp8_many = (int64_t)c->cfg.max_tokens * c->cfg.K > 64 * (int64_t)c->cfg.E;
   c->ws = nullptr;   // the workspace is larger now
   c->ws_bytes = 0;
   carve(c, nullptr);
@@ -230,7 +234,7 @@ extern "C" eb_status eb_bind_weights_fp8(eb_ctx* c, const void* w_gate, const fl
   c->s8_gate = s_gate;
   c->s8_up = s_up;
   c->s8_down = s_down;
-  eb_status s = ebi_ffn8_bind(c);
+  eb_status s = c->fp8_many ? ebi_ffn8_many_bind(c) : ebi_ffn8_few_bind(c);
   if (s != EB_OK) c->w8_gate = c->w8_up = c->w8_down = nullptr;
   else c->use_fp8 = true;
   return s;
@@ -241,6 +245,7 @@ extern "C" size_t eb_workspace_bytes(const eb_ctx* c) {
   eb_ctx tmp;
   tmp.cfg = c->cfg;
   tmp.fp8 = c->fp8;
+  tmp.fp8_many = c->fp8_many;
   return carve(&tmp, nullptr);
 }
 
@@ -278,7 +283,8 @@ extern "C" eb_status eb_expert_ffn_grouped_fp8(eb_ctx* c, void* stream, const vo
                                                const int32_t* group_w, const int32_t* step_meta, void* yp, int32_t device) {
   if (!c) return EB_ERR_INVALID_ARG;
   if (device >= c->cfg.D) return ebi_fail(c, EB_ERR_INVALID_ARG, "device out of range");
-  return ebi_ffn8_run(c, (cudaStream_t)stream, xq, xs, group_off, group_w, step_meta, yp, device < 0 ? -1 : device);
+  return (c->fp8_many ? ebi_ffn8_many_run : ebi_ffn8_few_run)(c, (cudaStream_t)stream, xq, xs, group_off, group_w, step_meta, yp,
+                                                              device < 0 ? -1 : device, false);
 }
 
 static eb_status check_buffers(eb_ctx* c, const eb_step_buffers* b) {
@@ -303,7 +309,8 @@ extern "C" eb_status eb_step(eb_ctx* c, void* stream, const eb_batch* batch, uin
   if (!c->ws) return ebi_fail(c, EB_ERR_WORKSPACE, "no workspace set");
   cudaStream_t st = (cudaStream_t)stream;
   if ((s = ebi_front_run(c, st, bp, batch->pool_mask, route_mask, m, policy, b)) != EB_OK) return s;
-  s = c->use_fp8 ? ebi_ffn8_run(c, st, b->xp, ebi_row_scales(c, b->xp), b->group_off, b->group_w, b->step_meta, b->yp, -1, true)
+  s = c->use_fp8 ? (c->fp8_many ? ebi_ffn8_many_run : ebi_ffn8_few_run)(c, st, b->xp, ebi_row_scales(c, b->xp), b->group_off, b->group_w, b->step_meta,
+                                                                        b->yp, -1, true)
                  : ebi_ffn_run(c, st, b->xp, b->group_off, b->group_w, b->step_meta, b->yp, -1, true);
   if (s != EB_OK) return s;
   if (!ebi_aligned16(b->residual)) return ebi_fail(c, EB_ERR_INVALID_ARG, "residual not 16-byte aligned");

@@ -743,14 +743,14 @@ int ebi_pair_grid(eb_ctx* c, const void* kernel, int threads, size_t smem) {
   return 2 * (clusters < c->num_sms / 2 ? clusters : c->num_sms / 2);
 }
 
-eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, bool fp8) {
+eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, EbPass pass) {
   {
     KernelTimer timer(c, EBK_FFN_PLAN, st);
-    EB_LAUNCH(c, "expert_ffn", ebi_launch(plan_kernel, dim3(1), dim3(1024), 0, st, c->mp, group_off, step_meta, (int)device, tile_plan_of(c, fp8)));
+    EB_LAUNCH(c, "expert_ffn", ebi_launch(plan_kernel, dim3(1), dim3(1024), 0, st, c->mp, group_off, step_meta, (int)device, tile_plan_of(c, pass)));
   }
   KernelTimer timer(c, EBK_FFN_FILL, st);
   EB_LAUNCH(c, "expert_ffn", ebi_launch(fill_kernel, dim3(c->num_sms), dim3(256), sizeof(int) * (size_t)(ebi_groups_cap(c) + 1), st, c->mp,
-                                        group_off, group_w, tile_list_of(c, fp8)));
+                                        group_off, group_w, tile_list_of(c, pass)));
   return EB_OK;
 }
 
@@ -802,7 +802,7 @@ eb_status ebi_ffn_run(eb_ctx* c, cudaStream_t st, const void* xp, const int32_t*
   p.I = g.I;
   p.status = c->d_status;
   if (!planned)
-    if (eb_status s = ebi_ffn_plan(c, st, group_off, group_w, step_meta, device, false)) return s;
+    if (eb_status s = ebi_ffn_plan(c, st, group_off, group_w, step_meta, device, EB_PASS_BF16)) return s;
   if (!c->timing) {
     p.part = 0;
     EB_LAUNCH(c, "expert_ffn", launch_ffn(c, st, p));

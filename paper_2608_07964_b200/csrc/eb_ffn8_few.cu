@@ -100,13 +100,30 @@ __device__ __forceinline__ void st_shared4(uint32_t addr, float a, float b, floa
   asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
 }
 
-// silu(g) * u.  Not by tanh.approx: its 2^-11 would send one value in a hundred to the other e4m3 neighbour.
-__device__ __forceinline__ float silu_mul_f32(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+__device__ __forceinline__ float exp2f_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// silu(g) * u for two values, sigmoid(g) = 1 / (1 + exp(-g)).  Not by tanh.approx: its 2^-11 would send one value in a hundred to
+// the other e4m3 neighbour.  The special function unit bounds the epilogue of a tile, so two quotients share one reciprocal: of the product, which
+// the exponents' limit of 2^60 keeps finite (a sigmoid below 2^-60 counts as that).
+__device__ __forceinline__ void silu_mul2(float g0, float u0, float g1, float u1, float* h0, float* h1) {
+  const float d0 = 1.f + exp2f_approx(fminf(g0 * -1.442695041f, 60.f)), d1 = 1.f + exp2f_approx(fminf(g1 * -1.442695041f, 60.f));
+  const float r = rcp_approx(d0 * d1);
+  *h0 = g0 * u0 * (r * d1);
+  *h1 = g1 * u1 * (r * d0);
+}
 
 struct TokenMaps8 {
   CUtensorMap box[4];   // 64 / 32 / 16 / 8 rows
 };
-struct Ffn8Params {
+struct FewParams {
   TokenMaps8 xq, act;
   CUtensorMap gate, up, down;        // weight boxes of 128 rows; with the above kMaps tensor maps in a row
   const float *xs, *s_gate, *s_up, *s_down;
@@ -123,7 +140,7 @@ struct Ffn8Params {
   int* status;
 };
 constexpr int kMaps = 11;
-static_assert(offsetof(Ffn8Params, down) == (kMaps - 1) * sizeof(CUtensorMap), "the maps are prefetched as an array");
+static_assert(offsetof(FewParams, down) == (kMaps - 1) * sizeof(CUtensorMap), "the maps are prefetched as an array");
 
 // The 32 columns a quadrant's two warps share go to them as 16-column chunks in turn: chunk i of a warp starts at column
 // first + 32 i.  acc[a][..]: sums of accumulator a, two columns a word.
@@ -153,7 +170,7 @@ __device__ __forceinline__ void add_block(Sums<NC>& s, uint32_t tmem, uint32_t s
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
-ffn8_kernel(const __grid_constant__ Ffn8Params p) {
+ffn8_few_kernel(const __grid_constant__ FewParams p) {
   EB_GRID_DEP_SYNC();
   constexpr int NS = kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -246,6 +263,22 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
     const int4 a = ld_shared(items + i * (uint32_t)sizeof(Tile)), b = ld_shared(items + i * (uint32_t)sizeof(Tile) + 16);
     *it = Tile{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     return true;
+  };
+  // The same for a whole warp: one lane takes it and frees the slot (a wait with cluster scope by all 32 takes 6000 cycles).
+  auto take_item_warp = [&](int seq, Tile* it) {
+    int ok = 1;
+    if (lane == 0) {
+      ok = take_item(seq, it) ? 1 : 0;
+      if (ok && it->w >= 0) mbar_arrive_cluster(map_to_cta(item_empty(seq % kItems), 1));
+    }
+    it->row = __shfl_sync(0xffffffffu, it->row, 0);
+    it->rows = __shfl_sync(0xffffffffu, it->rows, 0);
+    it->w = __shfl_sync(0xffffffffu, it->w, 0);
+    it->out = __shfl_sync(0xffffffffu, it->out, 0);
+    it->phase = __shfl_sync(0xffffffffu, it->phase, 0);
+    it->done = __shfl_sync(0xffffffffu, it->done, 0);
+    it->need = __shfl_sync(0xffffffffu, it->need, 0);
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
   };
   auto free_item = [&](int seq) { mbar_arrive_cluster(map_to_cta(item_empty(seq % kItems), 1)); };
 
@@ -414,11 +447,9 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
       // ---------------- scales: token's times weight block's, a turn at a time ----------------
       uint32_t turn = 0;
       for (int seq = 0;; ++seq) {
-        Tile it;
-        if (!__all_sync(0xffffffffu, take_item(seq, &it))) goto done;
+        Tile it = {};
+        if (!take_item_warp(seq, &it)) goto done;
         if (it.w < 0) break;
-        __syncwarp();
-        if (lane == 0) free_item(seq);
         const bool down = it.phase == 2;
         const int num_kb = down ? num_kb2 : num_kb1;
         const int width = turn_width(entry_cols(it.rows)), per = kMaxCols / width;
@@ -447,33 +478,44 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
         }
         if (down && it.need > 0) {
           const int* flag = p.ready + it.done;
-          if (!__all_sync(0xffffffffu, bounded_wait([&] { return ld_acquire(flag) >= it.need; }, s_abort, status))) goto done;
+          int ok = 1;   // one lane asks
+          if (lane == 0) ok = bounded_wait([&] { return ld_acquire(flag) >= it.need; }, s_abort, status) ? 1 : 0;
+          if (!__shfl_sync(0xffffffffu, ok, 0)) goto done;
+          __syncwarp();
         }
-        float x[4], w0, w1;
-        auto load = [&](int kb) {
+        // Those of four turns are on their way at a time: with one, a turn took as long as its trip to L2 (1000 cycles)
+        float x[4][4], w0[4], w1[4];
+        auto load = [&](int kb, float (&xk)[4], float& w0k, float& w1k) {
           if (kb >= num_kb) return;
-          w0 = __ldg(sw0 + kb);
-          w1 = __ldg(sw1 + kb);
+          w0k = __ldg(sw0 + kb);
+          w1k = __ldg(sw1 + kb);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             // the intermediate's scales were written by this launch: from L2
-            x[i] = down ? __ldcg(sx[i] + (size_t)kb * step) : __ldg(sx[i] + kb);
+            xk[i] = down ? __ldcg(sx[i] + (size_t)kb * step) : __ldg(sx[i] + kb);
           }
         };
-        load(g);
-        for (int kb0 = 0; kb0 < num_kb; kb0 += per, ++turn) {
-          const int slot = turn % kScaleSlots;
-          const float a0 = x[0] * w0, a1 = x[1] * w0, a2 = x[2] * w0, a3 = x[3] * w0;
-          const float b0 = x[0] * w1, b1 = x[1] * w1, b2 = x[2] * w1, b3 = x[3] * w1;
-          load(kb0 + per + g);
-          if (!__all_sync(0xffffffffu, mbar_wait(sempty_bar(slot), ((turn / kScaleSlots) & 1u) ^ 1u, s_abort, status))) goto done;
-          if (kb0 + g < num_kb) {
-            const uint32_t at = base + kScaleOff + 4u * (slot * kScaleFloats + g * 2 * width + tok);
-            st_shared4(at, a0, a1, a2, a3);
-            st_shared4(at + 4u * width, b0, b1, b2, b3);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load(j * per + g, x[j], w0[j], w1[j]);
+        for (int kb0 = 0; kb0 < num_kb; kb0 += 4 * per) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int kb = kb0 + j * per;
+            if (kb >= num_kb) break;
+            const int slot = turn % kScaleSlots;
+            int ok = 1;
+            if (lane == 0) ok = mbar_wait(sempty_bar(slot), ((turn / kScaleSlots) & 1u) ^ 1u, s_abort, status) ? 1 : 0;
+            if (!__shfl_sync(0xffffffffu, ok, 0)) goto done;
+            if (kb + g < num_kb) {
+              const uint32_t at = base + kScaleOff + 4u * (slot * kScaleFloats + g * 2 * width + tok);
+              st_shared4(at, x[j][0] * w0[j], x[j][1] * w0[j], x[j][2] * w0[j], x[j][3] * w0[j]);
+              st_shared4(at + 4u * width, x[j][0] * w1[j], x[j][1] * w1[j], x[j][2] * w1[j], x[j][3] * w1[j]);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(sfull_bar(slot));
+            ++turn;
+            load(kb + 4 * per + g, x[j], w0[j], w1[j]);
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive_release(sfull_bar(slot));
         }
       }
     } else {
@@ -505,11 +547,9 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
     uint8_t* const tile = smem + kTileOff + ew * 1024;
     uint32_t turn = 0, made = 0;   // made: gate/up tiles so far
     for (int seq = 0;; ++seq) {
-      Tile it;
-      if (!__all_sync(0xffffffffu, take_item(seq, &it))) goto done;
+      Tile it = {};
+      if (!take_item_warp(seq, &it)) goto done;
       if (it.w < 0) break;
-      __syncwarp();
-      if (lane == 0) free_item(seq);
       const int cols = entry_cols(it.rows), num_kb = it.phase == 2 ? num_kb2 : num_kb1;
       const bool merged = it.rows < 0;
       const int n_cols = merged ? -it.rows * kSlotRows : it.rows;   // columns that may hold rows to store
@@ -534,9 +574,9 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
           for (int i = 0; i < NC * 8; ++i) s.v[a][i] = 0;
         for (int kb0 = 0; kb0 < num_kb; kb0 += PER, ++turn) {
           const int h = turn & 1u, slot = turn % kScaleSlots, n = min(PER, num_kb - kb0);
-          bool ok = mbar_wait(sfull_bar(slot), (turn / kScaleSlots) & 1u, s_abort, status);
-          ok = ok && mbar_wait(tfull_bar(h), (turn >> 1) & 1u, s_abort, status);
-          if (!__all_sync(0xffffffffu, ok)) return false;
+          int ok = 1;   // one lane waits: a wait by all 32 takes 170 cycles
+          if (lane == 0) ok = mbar_wait(sfull_bar(slot), (turn / kScaleSlots) & 1u, s_abort, status) && mbar_wait(tfull_bar(h), (turn >> 1) & 1u, s_abort, status) ? 1 : 0;
+          if (!__shfl_sync(0xffffffffu, ok, 0)) return false;
           tc_fence_after();
           for (int g = 0; g < n; ++g)
             add_block<NC>(s, taddr + h * kTmemHalf + g * 2 * W, scale0 + 4u * (slot * kScaleFloats + g * 2 * W), W);
@@ -554,7 +594,9 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
 #pragma unroll
           for (int i = 0; i < NC * 8; ++i) {
             const float2 gt = unpack2(s.v[0][i]), up = unpack2(s.v[1][i]);
-            const uint32_t lo = __float_as_uint(silu_mul_f32(gt.x, up.x)), hi = __float_as_uint(silu_mul_f32(gt.y, up.y));
+            float h0, h1;
+            silu_mul2(gt.x, up.x, gt.y, up.y, &h0, &h1);
+            const uint32_t lo = __float_as_uint(h0), hi = __float_as_uint(h1);
             s.v[0][i] = pack2(lo, hi);
             const uint32_t ml = __reduce_max_sync(0xffffffffu, lo & 0x7fffffffu), mh = __reduce_max_sync(0xffffffffu, hi & 0x7fffffffu);
             if (lane == ((2 * i) & 31)) most[i / 16] = ml;
@@ -565,7 +607,9 @@ ffn8_kernel(const __grid_constant__ Ffn8Params p) {
           for (int k = 0; k < (NC + 1) / 2; ++k) mx[q * kMaxCols + 32 * k + lane] = most[k];
           __syncwarp();
           if (lane == 0) mbar_arrive_release(max_bar(side));
-          if (!__all_sync(0xffffffffu, mbar_wait(max_bar(side), made & 1u, s_abort, status))) return false;
+          int ok = 1;
+          if (lane == 0) ok = mbar_wait(max_bar(side), made & 1u, s_abort, status) ? 1 : 0;
+          if (!__shfl_sync(0xffffffffu, ok, 0)) return false;
           ++made;
 #pragma unroll
           for (int k = 0; k < (NC + 1) / 2; ++k) {
@@ -659,7 +703,7 @@ done:
   }
 }
 
-cudaError_t launch_ffn8(eb_ctx* c, cudaStream_t st, const Ffn8Params& p) {
+cudaError_t launch_few(eb_ctx* c, cudaStream_t st, const FewParams& p) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c->pair_grid8);
   cfg.blockDim = dim3(kThreads);
@@ -675,26 +719,26 @@ cudaError_t launch_ffn8(eb_ctx* c, cudaStream_t st, const Ffn8Params& p) {
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   ++g_ebi_launches;
-  return cudaLaunchKernelEx(&cfg, ffn8_kernel, p);
+  return cudaLaunchKernelEx(&cfg, ffn8_few_kernel, p);
 }
 
 }  // namespace
 
-eb_status ebi_ffn8_bind(eb_ctx* c) {
+eb_status ebi_ffn8_few_bind(eb_ctx* c) {
   if (eb_status ds = ebi_check_device(c)) return ds;
   const eb_config& g = c->cfg;
   const uint64_t nw = (uint64_t)g.L * (g.E + g.S);
   if (!make_map(&c->tm8_gate, c->w8_gate, g.H, g.I, nw, BK, 128, true) || !make_map(&c->tm8_up, c->w8_up, g.H, g.I, nw, BK, 128, true) ||
       !make_map(&c->tm8_down, c->w8_down, g.I, g.H, nw, BK, 128, true))
     return ebi_fail(c, EB_ERR_CUDA, "cuTensorMapEncodeTiled failed for the weights");
-  cudaError_t e = cudaFuncSetAttribute(ffn8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(ffn8_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   if (e != cudaSuccess) return ebi_check_cuda(c, e, "cudaFuncSetAttribute");
-  c->pair_grid8 = ebi_pair_grid(c, (const void*)ffn8_kernel, kThreads, kSmemBytes);
+  c->pair_grid8 = ebi_pair_grid(c, (const void*)ffn8_few_kernel, kThreads, kSmemBytes);
   if (!c->pair_grid8) return ebi_fail(c, EB_ERR_CUDA, "the device cannot hold a 2-CTA cluster of the 8-bit expert kernel");
   return EB_OK;
 }
 
-eb_status ebi_ffn8_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
+eb_status ebi_ffn8_few_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
                        const int32_t* step_meta, void* yp, int32_t device, bool planned) {
   if (!xq || !xs || !group_off || !group_w || !step_meta || !yp) return ebi_fail(c, EB_ERR_INVALID_ARG, "null pointer");
   if (eb_status ds = ebi_check_device(c)) return ds;
@@ -703,7 +747,7 @@ eb_status ebi_ffn8_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* 
   if (!c->ws) return ebi_fail(c, EB_ERR_WORKSPACE, "no workspace set");
   const eb_config& g = c->cfg;
   const int rows = ebi_rows_cap(c);
-  Ffn8Params p;
+  FewParams p;
   const int box_rows[4] = {64, 32, 16, 8};
   for (int i = 0; i < 4; ++i)
     if (!make_map(&p.xq.box[i], xq, g.H, rows, 0, BK, box_rows[i], true) || !make_map(&p.act.box[i], c->act, g.I, rows, 0, BK, box_rows[i], true))
@@ -728,19 +772,19 @@ eb_status ebi_ffn8_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* 
   p.rows_cap = rows;
   p.status = c->d_status;
   if (!planned)
-    if (eb_status s = ebi_ffn_plan(c, st, group_off, group_w, step_meta, device, true)) return s;
+    if (eb_status s = ebi_ffn_plan(c, st, group_off, group_w, step_meta, device, EB_PASS_FP8_FEW)) return s;
   if (!c->timing) {
     p.part = 0;
-    EB_LAUNCH(c, "expert_ffn_fp8", launch_ffn8(c, st, p));
+    EB_LAUNCH(c, "expert_ffn_fp8", launch_few(c, st, p));
   } else {   // the same tiles in two launches, so that each phase gets a time of its own
     {
       KernelTimer timer(c, EBK_FFN_GATEUP, st);
       p.part = 1;
-      EB_LAUNCH(c, "expert_ffn_fp8", launch_ffn8(c, st, p));
+      EB_LAUNCH(c, "expert_ffn_fp8", launch_few(c, st, p));
     }
     KernelTimer timer(c, EBK_FFN_DOWN, st);
     p.part = 2;
-    EB_LAUNCH(c, "expert_ffn_fp8", launch_ffn8(c, st, p));
+    EB_LAUNCH(c, "expert_ffn_fp8", launch_few(c, st, p));
   }
   EB_LAUNCH_CHECK(c, "expert_ffn_fp8");
   return EB_OK;

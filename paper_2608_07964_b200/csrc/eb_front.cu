@@ -618,7 +618,7 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
       EB_LAUNCH(c, "sums", ebi_launch(sums_kernel, dim3((seg.off[EB_MAX_MB] * g.E + 255) / 256), dim3(256), 0, st, c->mp, bp, seg, pool_mask | route_mask,
                                       (const int32_t*)c->chunk_hist, c->chunk_base, c->chunk_seg));
     const TablesArgs a{pool_mask, route_mask, (int)m, (int)policy, c->chunk_hist, sums ? c->chunk_seg : nullptr, c->chunk_base, c->seg_base,
-                       c->mb_base, b->mb_load, b->mb_cnt, seg, layers_of(bp), b->sched, b->group_off, b->group_w, b->step_meta, tile_plan_of(c, c->use_fp8),
+                       c->mb_base, b->mb_load, b->mb_cnt, seg, layers_of(bp), b->sched, b->group_off, b->group_w, b->step_meta, tile_plan_of(c, ebi_pass(c)),
                        sched_grid_of(c)};
     int blocks = sched_blocks(pool_mask, m, policy);
     if ((int64_t)sched_subsets(pool_mask, m) * (blocks - 1) / blocks < kSchedSubsets) blocks = 1;
@@ -635,7 +635,7 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
     const int members = __builtin_popcount(pool_mask), sure = policy == EB_POLICY_ALL ? members : std::min((int)m, members);
     const uint32_t touch_mask = 2 * sure >= members ? pool_mask : 0;
     const ScatterArgs a{b->sched, b->topk_idx, c->chunk_base, sums ? c->seg_base : nullptr, c->mb_base, b->group_off, b->group_w, seg, b->pos, b->row_src, b->step_meta,
-                        (const uint4*)b->x, (uint4*)b->xp, (uint2*)b->xp, ebi_row_scales(c, b->xp), tile_list_of(c, c->use_fp8), c->num_sms / 2, row_team(g.H / 8), touch_mask,
+                        (const uint4*)b->x, (uint4*)b->xp, (uint2*)b->xp, ebi_row_scales(c, b->xp), tile_list_of(c, ebi_pass(c)), c->num_sms / 2, row_team(g.H / 8), touch_mask,
                         b->mb_load, schedule_watch_of(c)};
     const size_t smem = sizeof(int) * (size_t)(ebi_groups_cap(c) + 1);
     auto launch = [&](auto kernel, int tb) {

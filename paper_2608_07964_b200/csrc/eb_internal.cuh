@@ -96,6 +96,7 @@ struct eb_ctx {
   CUtensorMap tm_gate, tm_up, tm_down, tm_gate64, tm_up64;
   // 8-bit expert path (eb_enable_fp8): e4m3 weights with a scale per 128 x 128 block
   bool fp8 = false;                // the workspace is laid out for it too
+  bool fp8_many = false;           // by which of its two kernels
   bool use_fp8 = false;            // the weights bound last are 8-bit ones
   const void *w8_gate = nullptr, *w8_up = nullptr, *w8_down = nullptr;
   const float *s8_gate = nullptr, *s8_up = nullptr, *s8_down = nullptr;
@@ -244,11 +245,17 @@ eb_status ebi_ffn_run(eb_ctx* c, cudaStream_t st, const void* xp, const int32_t*
 eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint32_t pool_mask, uint32_t route_mask, int32_t m,
                         eb_policy policy, const eb_step_buffers* b);
 eb_status ebi_ffn_bind(eb_ctx* c);
-// The same for 8-bit weights (eb_ffn8.cu); the tile list of an expert pass that is not planned (eb_ffn.cu).
-eb_status ebi_ffn8_bind(eb_ctx* c);
-eb_status ebi_ffn8_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
-                       const int32_t* step_meta, void* yp, int32_t device, bool planned = false);
-eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, bool fp8);
+// The same for 8-bit weights, two kernels; the tile list of an expert pass that is not planned (eb_ffn.cu).
+eb_status ebi_ffn8_few_bind(eb_ctx* c);
+eb_status ebi_ffn8_few_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
+                           const int32_t* step_meta, void* yp, int32_t device, bool planned);
+eb_status ebi_ffn8_many_bind(eb_ctx* c);
+eb_status ebi_ffn8_many_run(eb_ctx* c, cudaStream_t st, const void* xq, const float* xs, const int32_t* group_off, const int32_t* group_w,
+                            const int32_t* step_meta, void* yp, int32_t device, bool planned);
+enum EbPass { EB_PASS_BF16, EB_PASS_FP8_FEW, EB_PASS_FP8_MANY };
+// The expert pass of the weights bound last.
+inline EbPass ebi_pass(const eb_ctx* c) { return !c->use_fp8 ? EB_PASS_BF16 : c->fp8_many ? EB_PASS_FP8_MANY : EB_PASS_FP8_FEW; }
+eb_status ebi_ffn_plan(eb_ctx* c, cudaStream_t st, const int32_t* group_off, const int32_t* group_w, const int32_t* step_meta, int32_t device, EbPass pass);
 int ebi_pair_grid(eb_ctx* c, const void* kernel, int threads, size_t smem);
 // The host checks of a router; false: why not in *why.
 bool ebi_router_ok(const eb_config& g, const eb_router* r, RouterParams* out, const char** why);

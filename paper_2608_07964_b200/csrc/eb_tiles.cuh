@@ -6,11 +6,12 @@
 namespace {
 
 constexpr int kTileRows = 256;                                 // token rows of a tile at most
-constexpr int kTileShift = 8, kTileShift8 = 7;                 // as powers of two: bf16 tiles, 8-bit tiles (of 128 rows at most)
+constexpr int kTileShift = 8, kTileShiftFew = 7;               // as powers of two; 7: tiles of 8-bit weights for few rows
 constexpr int kFeat1 = 256;                                    // outputs of a gate/up tile
 constexpr int kFeat2 = 512;                                    // outputs of a down tile
+constexpr int kFeat1Many = 128, kFeat2Many = 256;              // of tiles of 8-bit weights for many rows
 constexpr int kSlotRows = 16;                                  // rows of one slot of a merged tile
-constexpr int kMergeSlots = kTileRows / kSlotRows;             // slots of a merged tile at most (8-bit tiles: half of them)
+constexpr int kMergeSlots = kTileRows / kSlotRows;             // slots of a merged tile at most (with tiles of 128 rows: half of them)
 constexpr int kMergeMaxRows = 64;                              // replicas of a shared expert are merged when none has more rows
 
 // Accumulator columns of a tile of `valid_rows` token rows: rounded up to 16 (each CTA of the pair supplies half
@@ -30,15 +31,15 @@ struct Tile {
   int rows;     // rows (1 .. 256); -n for a merged tile of n slots of 16 rows, slots[row ..): (first row, rows)
   int w;        // weight matrix; negative: the list has ended
   int out;      // output tile
-  int phase;    // 1: gate/up + SwiGLU (256 outputs per tile);  2: down (512 outputs per tile)
+  int phase;    // 1: gate/up + SwiGLU (256 outputs per tile, or 128);  2: down (512, or 256)
   int done;     // the token tile this one belongs to: entry of `ready`
   int need;     // phase 2: arrivals on that entry after which the rows of the intermediate are all written (0: they are)
   int once;     // no other token tile of the launch reads its matrix
 };
 static_assert(sizeof(Tile) == 32, "two 16-byte words");
 
-// A group of `rows` rows is cut into ceil(rows / 256) tiles (8-bit: 128) of nearly equal size, so no tile is a short
-// remainder that would still stream a whole weight tile.  shift: kTileShift or kTileShift8.
+// A group of `rows` rows is cut into ceil(rows / 256) tiles (or / 128) of nearly equal size, so no tile is a short
+// remainder that would still stream a whole weight tile.  shift: kTileShift or kTileShiftFew.
 __device__ __forceinline__ int group_tiles(int rows, int shift) { return (rows + (1 << shift) - 1) >> shift; }
 __device__ __forceinline__ int merge_slots(int shift) { return (1 << shift) / kSlotRows; }
 // Columns (token rows rounded up to 16) of the largest tile of a group; its cost class is that count in steps of 32.
@@ -266,7 +267,7 @@ __device__ __forceinline__ void fill_tiles(const ModelParams& mp, const int32_t*
     const int pos = order[lo], g = pgroup[pos], n_slots = pslots[pos];
     Tile it;
     if (n_slots >= 0) {
-      // tile m of a merged class holds the next 16 (8-bit: 8) slots of the class, replicas in device order
+      // tile m of a merged class holds the next 16 (or 8) slots of the class, replicas in device order
       const int most = merge_slots(l.shift), base = kMergeSlots * (s_pref[lo] + m);
       const int first = most * m, n_here = min(most, n_slots - first);
       if (list == 0 && n == 0) {
@@ -303,13 +304,14 @@ __device__ __forceinline__ void fill_tiles(const ModelParams& mp, const int32_t*
   }
 }
 
-// The context's tile tables as the planning and filling blocks take them, for the bf16 or the 8-bit expert pass.
-inline TilePlan tile_plan_of(const eb_ctx* c, bool fp8) {
-  const int nt1 = (c->cfg.I + kFeat1 - 1) / kFeat1, nt2 = (c->cfg.H + kFeat2 - 1) / kFeat2;
-  return TilePlan{c->pgroup, c->pslots, c->prank, c->order, c->tile_pref, c->work_count, nt1, nt2, fp8 ? kTileShift8 : kTileShift};
+// The context's tile tables as the planning and filling blocks take them, for one of the expert passes.
+inline TilePlan tile_plan_of(const eb_ctx* c, EbPass pass) {
+  const int f1 = pass == EB_PASS_FP8_MANY ? kFeat1Many : kFeat1, f2 = pass == EB_PASS_FP8_MANY ? kFeat2Many : kFeat2;
+  return TilePlan{c->pgroup, c->pslots, c->prank, c->order, c->tile_pref, c->work_count, (c->cfg.I + f1 - 1) / f1, (c->cfg.H + f2 - 1) / f2,
+                  pass == EB_PASS_FP8_FEW ? kTileShiftFew : kTileShift};
 }
-inline TileList tile_list_of(const eb_ctx* c, bool fp8) {
-  const TilePlan p = tile_plan_of(c, fp8);
+inline TileList tile_list_of(const eb_ctx* c, EbPass pass) {
+  const TilePlan p = tile_plan_of(c, pass);
   return TileList{c->pgroup, c->pslots, c->order, c->tile_pref, c->work_count, p.nt1, p.nt2, p.shift, c->max_work, (Tile*)c->work, c->tile_ready, c->slots};
 }
 
