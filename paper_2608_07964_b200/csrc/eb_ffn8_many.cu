@@ -64,7 +64,8 @@ constexpr int kMaxOff = kBarOff + 512;                         // [512] largest 
 constexpr int kScaleWarps = 2;
 constexpr int kScaleSlots = 12;                                // k-blocks whose scales may lie ready
 constexpr int kScaleOff = kMaxOff + 512 * 4;                   // [slots][128 rows] products of both scales, for either half of a warp's columns
-constexpr size_t kSmemBytes = (size_t)kScaleOff + kScaleSlots * kCtaRows * 8 + 1024 /*alignment slack*/;
+constexpr int kTileOff = kScaleOff + kScaleSlots * kCtaRows * 8;                // 2 KB an epilogue warp: rows on their way out
+constexpr size_t kSmemBytes = (size_t)kTileOff + kEpiWarps * 2048 + 1024 /*alignment slack*/;
 // D[tmem of both CTAs] (+)= A * B^T on e4m3 with M = 256 (128 rows of A per CTA), N from the descriptor, K = 32
 __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -545,7 +546,7 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
     const int q = warp & 3, part = (warp - kEpiWarp0) >> 2;   // lane quadrant; which of its two warps
     uint32_t* const s_max = reinterpret_cast<uint32_t*>(smem + kMaxOff);
-    const bool act_whole = (p.I & 31) == 0, yp_whole = ((uintptr_t)p.yp & 31) == 0;   // 32-byte pieces of rows lie on 32-byte boundaries
+    const bool act_whole = (p.I & 31) == 0;   // 32-byte pieces of its rows lie on 32-byte boundaries
     uint32_t block = 0;   // k-blocks so far
     QuarterTurn turn;
     for (int seq = 0;; ++seq) {
@@ -667,19 +668,42 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
           // this warp's part of the intermediate is written: the publisher counts the CTA's share of the tile
           __syncwarp();
           if (lane == 0) mbar_arrive_release(part_bar(seq % kParts));
-        } else if (row >= 0) {
+        } else {
+          // A thread's outputs are a piece of one row; stored as they are, every store of a warp touches 32 lines (a tile's end took 4700 cycles).
+          // By way of shared memory eight (four) lanes write 128 (64) bytes of a row: NC columns at a time, of 16 (32) rows.
+          constexpr int kLanes = NC / 8, kRowsAtOnce = 32 * 64 / (2 * NC), kRowBytes = 2 * NC;
+          const uint32_t mine_at = base + kTileOff + (warp - kEpiWarp0) * 2048;
           const int col = it.out * kFeat2Many + half * 128 + col_half;
-          bf16* const at = p.yp + (size_t)row * p.H + col;
 #pragma unroll
-          for (int i = 0; i < NC / 8; ++i) {
-            const int c = i < NC / 16 ? 16 * i : 64 + 16 * (i - NC / 16);
-            uint32_t v[8];
+          for (int a = 0; a < 2; ++a) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float2 a = unpack2(sum[i / (NC / 16)][8 * (i % (NC / 16)) + k]);
-              v[k] = pack_bf16(a.x, a.y);
+            for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+              const int lr = lane - r0;   // this lane's row of those
+              if (lr >= 0 && lr < kRowsAtOnce) {
+#pragma unroll
+                for (int ch = 0; ch < kLanes; ++ch) {
+                  uint32_t v[4];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    const float2 f = unpack2(sum[a][4 * ch + k]);
+                    v[k] = pack_bf16(f.x, f.y);
+                  }
+                  // 16-byte pieces in an order of their own in every row, so that neither side meets in a bank
+                  const uint32_t to = mine_at + lr * kRowBytes + ((ch ^ (NC == 64 ? lr : lr >> 1)) & (kLanes - 1)) * 16;
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                }
+              }
+              __syncwarp();
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int rr = j * (32 / kLanes) + lane / kLanes, ch = lane % kLanes;
+                const int4 v = ld_shared(mine_at + rr * kRowBytes + ((ch ^ (NC == 64 ? rr : rr >> 1)) & (kLanes - 1)) * 16);
+                const int to_row = __shfl_sync(0xffffffffu, row, r0 + rr);
+                const int c = col + 64 * a + 8 * ch;
+                if (to_row >= 0 && c < p.H) *reinterpret_cast<int4*>(p.yp + (size_t)to_row * p.H + c) = v;   // H is a multiple of 16
+              }
+              __syncwarp();
             }
-            if (col + c < p.H) store32(at + c, v, yp_whole);   // H is a multiple of 16
           }
         }
         return true;
