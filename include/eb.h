@@ -255,7 +255,8 @@ eb_status eb_expert_ffn_device(eb_ctx* ctx, void* stream, const void* xp, const 
  * v * 448 / m rounded to nearest even (0 for a block of zeros).  A block with an infinity or NaN gets the scale NaN, and so
  * does everything made from it.  H and I are multiples of 16. */
 
-/* Lays the context out for 8-bit weights as well.  After eb_create, before eb_workspace_bytes and eb_set_workspace (a workspace set before
+/* Lays the context out for 8-bit weights as well, for one of two kernels: by tiles of 128 rows where the largest batch, all of it at one
+ * layer, gives an expert at most 64 rows on average (max_tokens * K <= 64 E), by tiles of 256 otherwise.  After eb_create, before eb_workspace_bytes and eb_set_workspace (a workspace set before
  * has to be set again: it is larger now).  EB_ERR_UNSUPPORTED if H or I is no multiple of 16. */
 eb_status eb_enable_fp8(eb_ctx* ctx);
 

@@ -1,4 +1,4 @@
-// eb_expert_ffn_grouped_fp8: the grouped SwiGLU pass on e4m3 rows and weights with a scale per block of 128.
+// eb_expert_ffn_grouped_fp8 for contexts of many rows per expert: the grouped SwiGLU pass on e4m3 rows and weights with a scale per block of 128.
 //
 //   gate[r, i] = sum_b xs[r, b] sg[i / 128, b] (sum over the 128 h of block b of xq[r, h] Wg[i, h]);  up likewise
 //   a = silu(gate) * up;  as[r, j] = max |a| over block j of 128 outputs / 448;  aq = a / as as e4m3
@@ -11,29 +11,32 @@
 //
 // That is why the TOKENS are the M operand here (256 rows a pair, 128 a CTA; a tile holds up to 256 rows) and 256 weight rows the N
 // operand: a TMEM lane is a token, so the product of both scales is one number per thread and block, the largest magnitude of a token's
-// outputs is found within threads, and a thread's outputs are neighbours in memory.  With the weights as M, as in ffn_kernel, every
-// column has a scale of its own, which each thread reads from shared memory: 65536 rows over 66 matrices of 3 x 2048 x 1408 took
-// 1249 us that way.  Tiles with few rows waste tensor work instead: a k-block takes 512 cycles whatever the rows, in which the
-// pair streams 32 KB of weights, more than its share of the memory rate, so that streaming stays what bounds them.
+// outputs is found within threads, and a thread's outputs are neighbours in memory.  With the weights as M (eb_ffn8_few.cu) every
+// column has a scale of its own, which each thread reads from shared memory, and twice the MMAs have to be issued: 65536 rows over 66 matrices
+// of 3 x 2048 x 1408 take 924 us here and 1249 there, 8192 rows over 32 of 3 x 4096 x 14336 2680 and 3109; but 2048 rows over 191 of
+// 3 x 2048 x 1408 415 and 302, since a k-block costs much the same here however few its rows.
 //
 // A gate/up tile makes 128 outputs: each CTA brings 64 rows of W_gate and the same 64 of W_up as its half of the N operand, so
 // that columns 0..63 | 64..127 of accumulator half c are gate | up of outputs 64 c ..; a down tile makes 256.  A thread
-// holds 128 sums, which is why the epilogue warps take registers over from the others (setmaxnreg).
+// holds up to 128 sums, which is why the epilogue warps take registers over from the others (setmaxnreg).
 //
-// Per CTA: warp 0 = weights by TMA, 1 = MMA issuer (leader CTA) or tile dealer (the other), 2 = token rows by TMA and scales, 3 = publisher of
-// finished rows, 4..11 = epilogue, two per lane quadrant, each with half of the columns; those whose lanes hold no rows only pass
+// Per CTA: warp 0 = weights by TMA, 1 = MMA issuer (leader CTA) or tile dealer (the other), 2 = token rows by TMA, 3 = publisher of
+// finished rows, 4 = gate of the epilogue, 5 and 6 = scales, 8..15 = epilogue, two per lane quadrant; those whose lanes hold no rows only pass
 // the accumulators on.  A stage is 32 KB per CTA (weights | up to 128 token rows of one k-block); six stages.  One commit per k-block
 // frees its stage and hands its accumulator over.
 //
-// What bounds a k-block is the epilogue warps' chain of waits, so they have nothing else in it: warp 2 leaves the products of both
-// scales in shared memory, eight blocks deep, and the first columns of the next block are on their way while the last
-// ones of this are added.  A TMA box costs its issuing thread about 110 cycles, so token rows are one box (rounded up to a power of two: lanes
-// without rows may hold anything) or, in a merged tile, a box per lane.
+// What bounds it: a k-block of 256 rows takes 1230 cycles, of which the MMAs need 512.  TMEM holds two such accumulators, and each goes round a
+// chain: MMAs 512 (and 350 until their end is seen), read and added by the epilogue 610, handed back 400.  To keep that chain short the
+// epilogue loop has nothing but one barrier, two words of scales, loads and multiply-adds in it; waits, scales and hand-overs are other
+// warps' work.  Measured on the way: waits by all lanes of all warps 170 cycles each, a wait with cluster scope by 32 lanes 6000, scales
+// fetched one block ahead 1000 a block, sixteen epilogue warps or waits within them no better, 32 columns a load worse (spills).
+// Multiply-adds are what the epilogue spends its time on: without them (wrong results) the 924 us are 684.
 //
-// The 128 outputs of a gate/up tile are a block of the intermediate: its largest magnitude per token is exchanged between the two
-// warps of a quadrant.
+// A TMA box costs its issuing thread about 110 cycles, so token rows are one box (rounded up to a power of two: lanes without rows may hold
+// anything) or, in a merged tile, a box per lane.  The 128 outputs of a gate/up tile are a block of the intermediate: its largest magnitude per
+// token is exchanged between the warps that hold parts of the row.
 //
-// Every wait is bounded as in ffn_kernel.
+// Every wait on a barrier in memory is bounded as in ffn_kernel.
 #include <cstddef>
 #include <type_traits>
 
@@ -66,7 +69,9 @@ constexpr int kScaleSlots = 12;                                // k-blocks whose
 constexpr int kScaleOff = kMaxOff + 512 * 4;                   // [slots][128 rows] products of both scales, for either half of a warp's columns
 constexpr int kTileOff = kScaleOff + kScaleSlots * kCtaRows * 8;                // 2 KB an epilogue warp: rows on their way out
 constexpr size_t kSmemBytes = (size_t)kTileOff + kEpiWarps * 2048 + 1024 /*alignment slack*/;
-// D[tmem of both CTAs] (+)= A * B^T on e4m3 with M = 256 (128 rows of A per CTA), N from the descriptor, K = 32
+static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
+
+// D[tmem of both CTAs] (+)= A * B^T on e4m3 with M (half of its rows per CTA) and N from the descriptor, K = 32
 __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -78,14 +83,14 @@ __device__ __forceinline__ void umma_pair_e4m3(uint32_t d_tmem, uint64_t a_desc,
 // Instruction descriptor: fp32 accumulate, e4m3 A and B (format 0), both K-major; N = 256.
 __device__ __forceinline__ uint32_t instr_desc_e4m3(int m) { return (1u << 4) | ((256u >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 
-// Which part of TMEM a k-block's accumulator takes: two of four quarters (128 columns each), or one in a slim tile, in turn.  The MMA warp
+// Which part of TMEM a k-block's accumulator takes: two of four quarters (128 columns each), or one in a short tile, in turn.  The MMA warp
 // and the epilogue walk the same k-blocks and so reach the same placement and the same barrier phases.
 struct QuarterTurn {
   uint32_t next = 0, at = 0, phases = 15;   // phases, bit q: parity of the current use of quarter q (the first use has parity 0)
-  __device__ __forceinline__ void take(bool slim) {
-    at = slim ? next : ((next + 1) & 2u);
-    phases ^= (slim ? 1u : 3u) << at;
-    next = (at + (slim ? 1u : 2u)) & 3u;
+  __device__ __forceinline__ void take(bool is_short) {
+    at = is_short ? next : ((next + 1) & 2u);
+    phases ^= (is_short ? 1u : 3u) << at;
+    next = (at + (is_short ? 1u : 2u)) & 3u;
   }
   __device__ __forceinline__ uint32_t parity(uint32_t q) const { return (phases >> q) & 1u; }
 };
@@ -357,12 +362,12 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
           if (it.w < 0) break;
           free_item(seq);
           const int num_kb = it.phase == 2 ? num_kb2 : num_kb1;
-          const bool slim = short_tile(it);
-          const uint32_t idesc = instr_desc_e4m3(slim ? 128 : 256);
+          const bool is_short = short_tile(it);
+          const uint32_t idesc = instr_desc_e4m3(is_short ? 128 : 256);
           for (int kb = 0; kb < num_kb; ++kb) {
-            turn.take(slim);
+            turn.take(is_short);
             if (!mbar_wait(tempty_bar(turn.at), turn.parity(turn.at) ^ 1u, s_abort, status)) goto done;
-            if (!slim && !mbar_wait(tempty_bar(turn.at + 1), turn.parity(turn.at + 1) ^ 1u, s_abort, status)) goto done;
+            if (!is_short && !mbar_wait(tempty_bar(turn.at + 1), turn.parity(turn.at + 1) ^ 1u, s_abort, status)) goto done;
             if (!mbar_wait(full_bar(stage), phase, s_abort, status)) goto done;
             tc_fence_after();
             const uint64_t dw = smem_desc(w_addr(stage)), dt = smem_desc(t_addr(stage));
@@ -501,10 +506,10 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
         bar_arrive(kBarTile, kGateThreads);
         if (s_stop[0]) goto done;
         if (it.w < 0) break;
-        const bool slim = short_tile(it);
+        const bool is_short = short_tile(it);
         const int num_kb = it.phase == 2 ? num_kb2 : num_kb1;
         for (int kb = 0; kb < num_kb; ++kb, ++block) {
-          turn.take(slim);
+          turn.take(is_short);
           if (lane == 0 && !(mbar_wait(scale_bar(block % kScaleSlots), (block / kScaleSlots) & 1u, s_abort, status) &&
                              mbar_wait(done_bar(stage), phase, s_abort, status)))
             s_stop[1] = 1;
@@ -514,7 +519,7 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
           bar_sync(kBarRead, kGateThreads);
           if (lane == 0) {
             mbar_arrive_cluster(tempty0 + 8 * turn.at);
-            if (!slim) mbar_arrive_cluster(tempty0 + 8 * turn.at + 8);
+            if (!is_short) mbar_arrive_cluster(tempty0 + 8 * turn.at + 8);
             mbar_arrive_release(scale_free(block % kScaleSlots));
             if (kb == 0) free_item(seq);   // all have read it
           }
@@ -559,16 +564,16 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
         it = Tile{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
       }
       if (it.w < 0) break;
-      const bool down = it.phase == 2, slim = short_tile(it);
+      const bool down = it.phase == 2, is_short = short_tile(it);
       const int num_kb = down ? num_kb2 : num_kb1;
       // half: of the N operand's columns, the 64 + 64 (gate and up, or one run of 128) that come from CTA `half`.  Wide: the two warps of a quadrant
-      // take a half each; slim: lanes 64.. hold the second half of the rows in lanes 0.., the warps take 32 + 32 columns.
-      const int half = slim ? q >> 1 : part, tok = slim ? (q & 1) * 32 + lane : q * 32 + lane;
+      // take a half each; is_short: lanes 64.. hold the second half of the rows in lanes 0.., the warps take 32 + 32 columns.
+      const int half = is_short ? q >> 1 : part, tok = is_short ? (q & 1) * 32 + lane : q * 32 + lane;
       const int mine = cta_rows(it, rank);
       const bool busy = tok - lane < mine;   // else no rows in these lanes: the accumulators pass by
       if (!busy) {
         for (int kb = 0; kb < num_kb; ++kb, ++block) {
-          turn.take(slim);
+          turn.take(is_short);
           bar_sync(kBarReady, kGateThreads);
           if (s_stop[1]) goto done;
           bar_arrive(kBarRead, kGateThreads);
@@ -632,7 +637,7 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
               sum[0][i] = pack2(lo, hi);
               most = max(most, max(lo & 0x7fffffffu, hi & 0x7fffffffu));
             }
-            // a row's two parts (wide) or four (slim); the barriers of the next tile keep its writes behind these reads
+            // a row's two parts (wide) or four (is_short); the barriers of the next tile keep its writes behind these reads
             constexpr int kRows = NC == 64 ? 128 : 64, kAll = NC == 64 ? 2 : 4;
             uint32_t* const mx = s_max + tok;
             mx[(NC == 64 ? part : half * 2 + part) * kRows] = most;
@@ -708,7 +713,7 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
         }
         return true;
       };
-      if (!(slim ? run(std::integral_constant<int, 32>()) : run(std::integral_constant<int, 64>()))) goto done;
+      if (!(is_short ? run(std::integral_constant<int, 32>()) : run(std::integral_constant<int, 64>()))) goto done;
     }
   }
 

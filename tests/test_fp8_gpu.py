@@ -81,10 +81,10 @@ SHAPES = [dict(L=2, E=4, K=2, S=0, H=16, I=16, D=2), dict(L=3, E=7, K=3, S=2, H=
           dict(L=4, E=31, K=3, S=1, H=1008, I=720, D=5), dict(L=2, E=16, K=8, S=8, H=272, I=144, D=16), dict(L=3, E=64, K=6, S=2, H=2048, I=1408, D=8)]
 
 
-def make(shape, tokens, layers=None, seed=0, **more):
+def make(shape, tokens, layers=None, seed=0, capacity=0, **more):
     E, D = shape["E"], shape["D"]
     off = [0] + np.cumsum(tokens).tolist()
-    step = B.MoEStep(shape["L"], E, shape["K"], shape["S"], shape["H"], shape["I"], D, [e * D // E for e in range(E)], max(off[-1], 1), fp8=True, **more)
+    step = B.MoEStep(shape["L"], E, shape["K"], shape["S"], shape["H"], shape["I"], D, [e * D // E for e in range(E)], max(off[-1], 1, capacity), fp8=True, **more)
     batch = B.Batch(off, [j % shape["L"] for j in range(len(tokens))] if layers is None else layers)
     T = off[-1]
     step.x[:T] = normal((T, shape["H"]), seed + 1)
@@ -172,11 +172,21 @@ def fill_rows(step, R, seed):
 SIZES = [[1], [0, 3, 0, 17], [16, 15, 32, 31], [33, 64, 65, 1], [100, 128, 129, 0], [256, 257, 300, 96], [700, 5, 48, 112]]
 
 
+def expert_step(sizes, H, I, many):
+    """A context of one layer and one device for groups of these sizes, whose capacity chooses the kernel for few or for many rows an expert."""
+    R, E = sum(sizes), len(sizes)
+    if many:
+        return B.MoEStep(1, E, 1, 0, H, I, 1, [0] * E, max(R + 3, 64 * E + 1), fp8=True)
+    E = max(E, -(-(R + 3) // 64))
+    return B.MoEStep(1, E, 1, 0, H, I, 1, [0] * E, R + 3, fp8=True)
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["few", "many"])
 @pytest.mark.parametrize("sizes", SIZES, ids=str)
 @pytest.mark.parametrize("H,I", [(16, 16), (128, 128), (144, 272), (512, 256), (1008, 720), (2048, 1408), (640, 4112)])
-def test_expert_pass(H, I, sizes):
+def test_expert_pass(H, I, sizes, many):
     R = sum(sizes)
-    step = B.MoEStep(1, len(sizes), 1, 0, H, I, 1, [0] * len(sizes), R + 3, fp8=True)
+    step = expert_step(sizes, H, I, many)
     get = weights8(step, H + I)
     assert table_of(step, sizes) == R
     fill_rows(step, R, 7)
@@ -194,10 +204,11 @@ def test_expert_pass(H, I, sizes):
         assert torch.equal(step.yp[:R], first)          # whatever the order of the tiles
 
 
-def test_scales_that_differ_from_block_to_block():
+@pytest.mark.parametrize("most", [128, 1000])   # rows of the context: the kernel for few rows an expert, for many
+def test_scales_that_differ_from_block_to_block(most):
     """Scales over many powers of two: a block whose scale were taken for another's would stand out."""
-    H, I, sizes = 1024, 640, [40, 200]
-    step = B.MoEStep(1, 2, 1, 0, H, I, 1, [0, 0], sum(sizes), fp8=True)
+    H, I, sizes = 1024, 640, [40, 88] if most == 128 else [40, 200]
+    step = B.MoEStep(1, 2, 1, 0, H, I, 1, [0, 0], most, fp8=True)
     gen = torch.Generator(device="cuda").manual_seed(11)
     e4m3 = lambda *s: (torch.randn(s, generator=gen, device="cuda") * 100).clamp(-448, 448).to(FP8)  # noqa: E731
     wide = lambda mid, *s: mid * torch.exp2(8 * torch.rand(s, generator=gen, device="cuda") - 4)      # noqa: E731
@@ -209,9 +220,10 @@ def test_scales_that_differ_from_block_to_block():
     check_groups(step, lambda i: [(q[0, i], s[0, i]) for q, s in w])
 
 
-def test_zeros_and_what_is_not_finite():
+@pytest.mark.parametrize("most", [128, 1000])
+def test_zeros_and_what_is_not_finite(most):
     H, I, sizes = 256, 384, [6, 70]
-    step = B.MoEStep(1, 2, 1, 0, H, I, 1, [0, 0], sum(sizes), fp8=True)
+    step = B.MoEStep(1, 2, 1, 0, H, I, 1, [0, 0], most, fp8=True)
     get = weights8(step, 2)
     R = table_of(step, sizes)
     fill_rows(step, R, 3)
@@ -227,12 +239,13 @@ def test_zeros_and_what_is_not_finite():
     within(step.yp[good], *R64.ffn(step.xq[good], step.xs[good], *get(1)))
 
 
+@pytest.mark.parametrize("capacity", [0, 1 << 12], ids=["few", "many"])
 @pytest.mark.parametrize("tokens", [[1, 1, 1], [4, 30, 9], [64, 64], [150, 500, 31]])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"E{s['E']}H{s['H']}")
-def test_steps_with_shared_experts_and_a_router(shape, tokens):
+def test_steps_with_shared_experts_and_a_router(shape, tokens, capacity):
     """Router, schedule, quantising dispatch, expert pass and aggregation as they are used together: by the calls one by one against the
     plain forms, then as whole steps, in place, from a graph and on another stream, bit for bit."""
-    step, batch, T = make(shape, tokens)
+    step, batch, T = make(shape, tokens, capacity=capacity)
     get = weights8(step, 9)
     bias = 0.3 * normal((shape["L"], shape["E"]), 4, dtype=torch.float32)
     router = B.Router("sigmoid", bias, scale=2.0)
@@ -327,6 +340,26 @@ def test_deferred_micro_batches_are_left_alone():
     assert step.check_permutation(batch) == 0
 
 
+@pytest.mark.parametrize("capacity", [0, 1 << 12], ids=["few", "many"])
+def test_two_contexts_and_streams_at_once(capacity):
+    """Contexts of their own on streams of their own: what they compute does not depend on each other."""
+    shape = SHAPES[3]
+    made = [make(shape, [60, 33, 90], seed=k, capacity=capacity) for k in (0, 10)]
+    streams, want = [torch.cuda.Stream() for _ in made], []
+    for step, batch, T in made:
+        weights8(step, 9)
+        step.eb_step(batch, 1, B.POLICY_ALL)
+        want.append(step.out[:T].clone())
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (step, batch, T), s in zip(made, streams):
+            with torch.cuda.stream(s):
+                step.eb_step(batch, 1, B.POLICY_ALL)
+    torch.cuda.synchronize()
+    for (step, batch, T), w in zip(made, want):
+        assert torch.equal(step.out[:T], w) and step.device_status() == 0 and step.check_workspace_guards() == 0
+
+
 def test_host_steps_and_runs_use_the_weights_bound_last():
     from paper_2608_07964_b200 import driver
     wl = synth.workload("c1")
@@ -338,6 +371,7 @@ def test_host_steps_and_runs_use_the_weights_bound_last():
     lg, x = synth.packed_logits(wl), synth.packed_hidden(wl)
     batch = B.Batch(wl.tok_off, wl.layers)
     h_out = torch.zeros((T, wl.H), dtype=torch.bfloat16).pin_memory()
+    step.out.zero_()                          # rows of the deferred micro-batch are left as they are, and compared too
     res = step.eb_step_host(batch, wl.m, lg.pin_memory(), x.pin_memory(), h_out)
     step.logits[:T], step.x[:T] = lg.cuda(), x.cuda()
     step.eb_step(batch, wl.m)
