@@ -43,7 +43,7 @@ constexpr int kStageBytes = 2 * kWBytes + kTBytes;             // W0 | W1 | toke
 constexpr int kRingBytes = kStages * kStageBytes;
 constexpr int kEpiWarp0 = 4, kEpiWarps = 8;                    // two per TMEM lane quadrant
 constexpr int kThreads = 32 * (kEpiWarp0 + kEpiWarps);
-constexpr int kRegsOther = 88, kRegsEpi = 208;                 // registers a thread after the split
+constexpr int kRegsOther = 72, kRegsEpi = 216;                 // registers a thread after the split
 static_assert(128 * kRegsOther + 256 * kRegsEpi <= kThreads * 168, "the split draws on what the block was launched with");
 constexpr int kTmemCols = 512, kTmemHalf = 256;
 constexpr int kMaxCols = 128;                                  // token columns of a tile
@@ -486,8 +486,9 @@ ffn8_few_kernel(const __grid_constant__ FewParams p) {
           if (!__shfl_sync(0xffffffffu, ok, 0)) goto done;
           __syncwarp();
         }
-        // Those of four turns are on their way at a time: with one, a turn took as long as its trip to L2 (1000 cycles)
-        float x[4][4], w0[4], w1[4];
+        // Those of two turns are on their way at a time: with one, a turn takes as long as its trip to L2 (1000 cycles); four cost spills (2 % at
+        // 2048 rows over 191 matrices)
+        float x[2][4], w0[2], w1[2];
         auto load = [&](int kb, float (&xk)[4], float& w0k, float& w1k) {
           if (kb >= num_kb) return;
           w0k = __ldg(sw0 + kb);
@@ -499,10 +500,10 @@ ffn8_few_kernel(const __grid_constant__ FewParams p) {
           }
         };
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load(j * per + g, x[j], w0[j], w1[j]);
-        for (int kb0 = 0; kb0 < num_kb; kb0 += 4 * per) {
+        for (int j = 0; j < 2; ++j) load(j * per + g, x[j], w0[j], w1[j]);
+        for (int kb0 = 0; kb0 < num_kb; kb0 += 2 * per) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 2; ++j) {
             const int kb = kb0 + j * per;
             if (kb >= num_kb) break;
             const int slot = turn % kScaleSlots;
@@ -517,7 +518,7 @@ ffn8_few_kernel(const __grid_constant__ FewParams p) {
             __syncwarp();
             if (lane == 0) mbar_arrive_release(sfull_bar(slot));
             ++turn;
-            load(kb + 4 * per + g, x[j], w0[j], w1[j]);
+            load(kb + 2 * per + g, x[j], w0[j], w1[j]);
           }
         }
       }

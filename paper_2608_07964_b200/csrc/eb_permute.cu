@@ -461,29 +461,36 @@ gather_kernel(int n_tok, int H, int KS, int team, const uint4* __restrict__ x, c
   }
 }
 
-// The same with the rows as e4m3 values and a scale for each block of 128 elements: the row is read and quantised once.
+// The same with the rows as e4m3 values and a scale for each block of 128 elements: the row is read and quantised once.  Sixteen elements a
+// thread (H is a multiple of 16), so that its K + S stores are 16 bytes each.
 __global__ void __launch_bounds__(kGatherThreads)
 gather_quant_kernel(int n_tok, int H, int KS, int team, const uint4* __restrict__ x, const int32_t* __restrict__ pos,
-                    uint2* __restrict__ xq, float* __restrict__ xs) {
+                    uint4* __restrict__ xq, float* __restrict__ xs) {
   EB_GRID_DEP_SYNC();
   const int t = blockIdx.x * (kGatherThreads / team) + threadIdx.x / team;
   if (t >= n_tok) return;
   const int lane = threadIdx.x & 31;
   const int my_pos = lane < KS ? pos[(size_t)t * KS + lane] : -1;
   if (!__any_sync(0xffffffffu, my_pos >= 0)) return;
-  const int vec = H / 8, blocks = ebi_blocks(H);
-  const uint4* src = x + (size_t)t * vec;
+  const int vec = H / 16, blocks = ebi_blocks(H);
+  const uint4* src = x + (size_t)t * (2 * vec);
   for (int v0 = 0; v0 < vec; v0 += team) {
     const int v = v0 + threadIdx.x % team;
-    uint4 r = make_uint4(0, 0, 0, 0);
-    if (v < vec) r = __ldg(src + v);
-    const BlockScale sc = warp_block_scale(r, team);
-    const uint2 q = quantise8(sc, r);
+    uint4 r[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (v < vec) {
+      r[0] = __ldg(src + 2 * v);
+      r[1] = __ldg(src + 2 * v + 1);
+    }
+    unsigned m = max(abs_max8(r[0]), abs_max8(r[1]));   // eight lanes hold a block
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const BlockScale sc = block_scale(m);
+    const uint2 lo = quantise8(sc, r[0]), hi = quantise8(sc, r[1]);
     for (int s = 0; s < KS; ++s) {
       const int p = __shfl_sync(0xffffffffu, my_pos, s);
       if (v < vec && p >= 0) {
-        xq[(size_t)p * vec + v] = q;
-        if ((v & 15) == 0) xs[(size_t)p * blocks + (v >> 4)] = sc.scale;
+        xq[(size_t)p * vec + v] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        if ((v & 7) == 0) xs[(size_t)p * blocks + (v >> 3)] = sc.scale;
       }
     }
   }
@@ -542,10 +549,10 @@ static eb_status permute_run(eb_ctx* c, void* stream, const eb_batch* batch, con
   }
   if (bp.n_tok > 0) {
     KernelTimer timer(c, EBK_PERMUTE_GATHER, st);
-    const int team = team_for(c->cfg.H / 8), tpb = kGatherThreads / team;
+    const int team = team_for(c->cfg.H / (quant ? 16 : 8)), tpb = kGatherThreads / team;
     if (quant)
       EB_LAUNCH(c, "permute", ebi_launch(gather_quant_kernel, dim3((bp.n_tok + tpb - 1) / tpb), dim3(kGatherThreads), 0, st, bp.n_tok, c->cfg.H,
-                                         c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint2*)xp, xs));
+                                         c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint4*)xp, xs));
     else
       EB_LAUNCH(c, "permute", ebi_launch(gather_kernel, dim3((bp.n_tok + tpb - 1) / tpb), dim3(kGatherThreads), 0, st, bp.n_tok, c->cfg.H,
                                          c->cfg.K + c->cfg.S, team, (const uint4*)x, (const int32_t*)pos, (uint4*)xp));
