@@ -121,17 +121,29 @@ __device__ __forceinline__ bool keep_groups(const RouterParams& rp, int E, int l
     last = top;
   }
   const bool sure = !last || apart(last, warp_max(value), 2.f * off);
+  if (size % 32 == 0) {   // no divisions: a register holds experts of one group
+    int left = size;
 #pragma unroll
-  for (int i = 0; i < PL; ++i)
-    if (!((kept >> min((lane + 32 * i) / size, 31)) & 1u)) key[i] = 0;
+    for (int i = 0; i < PL; ++i) {
+      if (!(kept & 1u)) key[i] = 0;
+      left -= 32;
+      if (left == 0) {
+        kept >>= 1;
+        left = size;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      if (!((kept >> min((lane + 32 * i) / size, 31)) & 1u)) key[i] = 0;
+  }
   return sure;
 }
 
-// The K best keys: expert number `lane` and its logit in lanes below K (-1: none left).  *sure: false if keys of 32 bits leave their order open.
+// The K best keys: expert number `lane` in lanes below K (-1: none left).  *sure: false if keys of 32 bits leave their order open.
 template <int PL, typename Key>
-__device__ __forceinline__ int choose(int K, int lane, Key (&key)[PL], const float (&z)[PL], float* my_z, float off, bool* sure) {
+__device__ __forceinline__ int choose(int K, int lane, Key (&key)[PL], float off, bool* sure) {
   int my_e = -1;
-  float mine = 0.f;
   Key last = 0;
   const int rounds = off > 0.f ? K + 1 : K;   // with the first that is not chosen
   for (int k = 0; k < rounds; ++k) {
@@ -143,17 +155,8 @@ __device__ __forceinline__ int choose(int K, int lane, Key (&key)[PL], const flo
     }
     if (!top || k == K) break;
     last = top;
-    float v = 0.f;
-#pragma unroll
-    for (int i = 0; i < PL; ++i)
-      if (lane + 32 * i == e) v = z[i];
-    v = __shfl_sync(0xffffffffu, v, e & 31);
-    if (lane == k) {
-      my_e = e;
-      mine = v;
-    }
+    if (lane == k) my_e = e;
   }
-  *my_z = mine;
   return my_e;
 }
 
@@ -171,7 +174,7 @@ __device__ __forceinline__ float warp_largest(float v) {
 // The choice with all sums in 64 bits.  Out of line: few tokens need it.
 template <int PL>
 __device__ __noinline__ int choose_exactly(const ModelParams& mp, const RouterParams& rp, const float* __restrict__ bias, int lane, const float (&z)[PL],
-                                           float z_top, float* my_z) {
+                                           float z_top) {
   double p[PL], sum = 0.0;
 #pragma unroll
   for (int i = 0; i < PL; ++i) {
@@ -193,7 +196,7 @@ __device__ __noinline__ int choose_exactly(const ModelParams& mp, const RouterPa
   }
   bool sure = true;
   if (rp.n_group > 1) keep_groups<PL>(rp, mp.E, lane, key, -1.f);
-  return choose<PL>(mp.K, lane, key, z, my_z, 0.f, &sure);
+  return choose<PL>(mp.K, lane, key, 0.f, &sure);
 }
 
 // Routes token t (E <= 32 PL), whose logits are zs[0 .. E): writes its row of topk_idx and topk_w.  Returns expert number `lane` in lanes
@@ -215,14 +218,13 @@ __device__ __forceinline__ int route_scored(const ModelParams& mp, const RouterP
     z_top = warp_largest(z_top);
   }
   int my_e = -1;
-  float my_z = 0.f;
   bool sure = true;
   if (!rp.bias && (rp.n_group == 1 || rp.group_top == 1)) {
     unsigned key[PL];
 #pragma unroll
     for (int i = 0; i < PL; ++i) key[i] = z[i] > -INFINITY ? float_key(z[i]) : 0u;
     if (rp.n_group > 1) keep_groups<PL>(rp, E, lane, key, -1.f);
-    my_e = choose<PL>(K, lane, key, z, &my_z, 0.f, &sure);
+    my_e = choose<PL>(K, lane, key, 0.f, &sure);
   } else {
     const float* const bias = rp.bias ? rp.bias + (size_t)layer * E : nullptr;
     float b[PL], p[PL], sum = 0.f;
@@ -245,11 +247,12 @@ __device__ __forceinline__ int route_scored(const ModelParams& mp, const RouterP
     }
     constexpr float kOff = 0x1p-18f;
     if (rp.n_group > 1) sure = keep_groups<PL>(rp, E, lane, key, kOff);
-    if (sure) my_e = choose<PL>(K, lane, key, z, &my_z, kOff, &sure);
-    if (!sure) my_e = choose_exactly<PL>(mp, rp, bias, lane, z, z_top, &my_z);
+    if (sure) my_e = choose<PL>(K, lane, key, kOff, &sure);
+    if (!sure) my_e = choose_exactly<PL>(mp, rp, bias, lane, z, z_top);
   }
   // weights: the scores, over their sum with the power of e that the largest chosen one holds taken out, so that no sum vanishes
   const bool there = lane < K && my_e >= 0;
+  const float my_z = there ? fminf(logit_value(zs[my_e]), FLT_MAX) : 0.f;   // a line at hand; carrying it along costs more
   float w;
   if (rp.sigmoid) {
     const float shift = mp.renorm ? fminf(warp_largest(there ? my_z : -INFINITY), 0.f) : 0.f;
