@@ -8,8 +8,8 @@
 // token's experts.  Without a bias c_e orders like z_e, so the logits are compared (integers in the order of the floats).  A sum, of a
 // bias or of two scores, is made and compared in 32 bits first, with a bound on how far it may be off: s_e = 1 / (1 + expf(-z)) is within 2^-21,
 // expf(z - top) / sum of at most 256 terms within 2^-19 (e^-d (d + 16) 2^-24, d = top - z), and the sum adds 2^-24 of its size.  Where neighbours of the
-// order, or the last group that stays and the first that goes, lie nearer than both bounds, the token is done again in 64 bits: about one token
-// in a hundred with 256 experts.  In 64 bits throughout, 65536 tokens took 389 us.
+// order, or the last group that stays and the first that goes, lie nearer than both bounds, the token is done again in 64 bits.
+// 65536 tokens, 256 experts in 8 groups: 389 us in 64 bits throughout, 205 this way.
 #pragma once
 
 #include <cfloat>
@@ -86,7 +86,7 @@ __device__ __forceinline__ bool keep_groups(const RouterParams& rp, int E, int l
     }
     if (lane == g) value = top;
   };
-  if (size % 32 == 0) {   // whole registers of all lanes: those 65536 tokens, eight groups of 32 experts, took 265 us by the other way, 208 by this
+  if (size % 32 == 0) {   // whole registers of all lanes: those 65536 tokens took 265 us by the other way when they took 208 by this
     Key a = 0, b = 0;
     int g = 0, left = size;
 #pragma unroll
