@@ -23,11 +23,10 @@
 
 namespace {
 
-// kScored: by scores, groups and a bias (eb_scores.cuh)
-template <int PL, bool kScored>
-__global__ void __launch_bounds__(kChunkThreads, PL <= 2 && !kScored ? 2 : 1)
-front_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
-             int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ chunk_hist) {
+// One chunk; route(t, j, lane): token t of micro-batch j.
+template <typename Route>
+__device__ __forceinline__ void front_chunk(const ModelParams& mp, const BatchParams& bp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
+                                            int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ chunk_hist, Route route) {
   __shared__ int s_hist[EB_MAX_E];
   const int c = blockIdx.x, j = mb_of_chunk(bp, c);
   const int t = bp.tok_off[j] + (c - bp.chunk_off[j]) * 32 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // a warp per token
@@ -39,11 +38,26 @@ front_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t pool_mask
   }
   EB_GRID_DEP_SYNC();
   if (!counted) return;
-  route_chunk(mp, bp, c, j, routed, topk_idx, s_hist, [&](int t) {
-    if constexpr (kScored) return route_scored<PL>(mp, rp, t, bp.layer[j], lane, logits + (size_t)t * mp.E, topk_idx, topk_w);
-    else return route_token<PL>(mp, t, lane, logits, topk_idx, topk_w);
-  });
+  route_chunk(mp, bp, c, j, routed, topk_idx, s_hist, [&](int t) { return route(t, j, lane); });
   for (int e = threadIdx.x; e < mp.E; e += kChunkThreads) chunk_hist[(size_t)c * mp.E + e] = s_hist[e];
+}
+
+template <int PL>
+__global__ void __launch_bounds__(kChunkThreads, PL <= 2 ? 2 : 1)
+front_kernel(ModelParams mp, BatchParams bp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
+             int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ chunk_hist) {
+  front_chunk(mp, bp, pool_mask, route_mask, logits, topk_idx, topk_w, chunk_hist,
+              [&](int t, int, int lane) { return route_token<PL>(mp, t, lane, logits, topk_idx, topk_w); });
+}
+
+// The same by scores, groups and a bias (eb_scores.cuh).
+template <int PL>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+front_scored_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t pool_mask, uint32_t route_mask, const float* __restrict__ logits,
+                    int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ chunk_hist) {
+  front_chunk(mp, bp, pool_mask, route_mask, logits, topk_idx, topk_w, chunk_hist, [&](int t, int j, int lane) {
+    return route_scored<PL>(mp, rp, t, bp.layer[j], lane, logits + (size_t)t * mp.E, topk_idx, topk_w);
+  });
 }
 
 // Running sum of n values that lie `stride` apart, left before each in `base` if `keep`; returns the total.  Sixteen loads at
@@ -601,10 +615,14 @@ eb_status ebi_front_run(eb_ctx* c, cudaStream_t st, const BatchParams& bp, uint3
   }
   if (bp.n_chunks > 0) {
     KernelTimer timer(c, EBK_ROUTE, st);
-    auto kernel = c->scored ? (g.E <= 64 ? front_kernel<2, true> : front_kernel<kMaxPerLane, true>)
-                            : (g.E <= 64 ? front_kernel<2, false> : front_kernel<kMaxPerLane, false>);
-    EB_LAUNCH(c, "front", ebi_launch(kernel, dim3(bp.n_chunks), dim3(kChunkThreads), 0, st, c->mp, bp, c->router,
-                                     pool_mask, route_mask, (const float*)b->logits, b->topk_idx, b->topk_w, c->chunk_hist));
+    const dim3 grid(bp.n_chunks), block(kChunkThreads);
+    const float* const logits = b->logits;
+    if (c->scored)
+      EB_LAUNCH(c, "front", ebi_launch(g.E <= 64 ? front_scored_kernel<2> : front_scored_kernel<kMaxPerLane>, grid, block, 0, st, c->mp, bp, c->router,
+                                       pool_mask, route_mask, logits, b->topk_idx, b->topk_w, c->chunk_hist));
+    else
+      EB_LAUNCH(c, "front", ebi_launch(g.E <= 64 ? front_kernel<2> : front_kernel<kMaxPerLane>, grid, block, 0, st, c->mp, bp, pool_mask, route_mask,
+                                       logits, b->topk_idx, b->topk_w, c->chunk_hist));
   }
   Segments seg;
   seg.off[0] = 0;

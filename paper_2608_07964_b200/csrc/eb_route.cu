@@ -10,28 +10,43 @@
 
 namespace {
 
-// kKind 0: softmax top-k on the logits; 1: by scores, groups and a bias (eb_scores.cuh), f32 logits; 2: the same, bf16 logits
-template <int PL, int kKind>
-__global__ void __launch_bounds__(kChunkThreads, PL <= 2 && kKind == 0 ? 2 : 1)
-route_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t route_mask, const void* __restrict__ logits, int64_t stride,
-             int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ mb_load,
-             int32_t* __restrict__ mb_cnt) {
-  EB_GRID_DEP_SYNC();
-  __shared__ int s_hist[EB_MAX_E], s_load[EB_MAX_D];
-  const int c = blockIdx.x, j = mb_of_chunk(bp, c), tid = threadIdx.x, lane = tid & 31;
-  if (!((route_mask >> j) & 1u)) return;
-  if (tid < mp.D) s_load[tid] = 0;
-  route_chunk(mp, bp, c, j, true, topk_idx, s_hist, [&](int t) {
-    if constexpr (kKind == 0) return route_token<PL>(mp, t, lane, (const float*)logits, topk_idx, topk_w);
-    else if constexpr (kKind == 1) return route_scored<PL>(mp, rp, t, bp.layer[j], lane, (const float*)logits + t * stride, topk_idx, topk_w);
-    else return route_scored<PL>(mp, rp, t, bp.layer[j], lane, (const bf16*)logits + t * stride, topk_idx, topk_w);
-  });
+// The chunk's counts, gathered in s_hist, to the loads.  s_load [D] is clear.
+__device__ __forceinline__ void add_loads(const ModelParams& mp, int j, const int* s_hist, int* s_load, int32_t* __restrict__ mb_load, int32_t* __restrict__ mb_cnt) {
+  const int tid = threadIdx.x;
   if (tid < mp.E && s_hist[tid] > 0) {
     atomicAdd(&mb_cnt[j * mp.E + tid], s_hist[tid]);
     atomicAdd(&s_load[mp.e2d[tid]], s_hist[tid]);
   }
   __syncthreads();
   if (tid < mp.D && s_load[tid] > 0) atomicAdd(&mb_load[j * mp.D + tid], s_load[tid]);
+}
+
+template <int PL>
+__global__ void __launch_bounds__(kChunkThreads, PL <= 2 ? 2 : 1)
+route_kernel(ModelParams mp, BatchParams bp, uint32_t route_mask, const float* __restrict__ logits,
+             int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ mb_load,
+             int32_t* __restrict__ mb_cnt) {
+  EB_GRID_DEP_SYNC();
+  __shared__ int s_hist[EB_MAX_E], s_load[EB_MAX_D];
+  const int c = blockIdx.x, j = mb_of_chunk(bp, c), lane = threadIdx.x & 31;
+  if (!((route_mask >> j) & 1u)) return;
+  if (threadIdx.x < mp.D) s_load[threadIdx.x] = 0;
+  route_chunk(mp, bp, c, j, true, topk_idx, s_hist, [&](int t) { return route_token<PL>(mp, t, lane, logits, topk_idx, topk_w); });
+  add_loads(mp, j, s_hist, s_load, mb_load, mb_cnt);
+}
+
+// The same by scores, groups and a bias (eb_scores.cuh); Z: float or bf16.
+template <int PL, typename Z>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+route_scored_kernel(ModelParams mp, BatchParams bp, RouterParams rp, uint32_t route_mask, const Z* __restrict__ logits, int64_t stride,
+                    int32_t* __restrict__ topk_idx, float* __restrict__ topk_w, int32_t* __restrict__ mb_load, int32_t* __restrict__ mb_cnt) {
+  EB_GRID_DEP_SYNC();
+  __shared__ int s_hist[EB_MAX_E], s_load[EB_MAX_D];
+  const int c = blockIdx.x, j = mb_of_chunk(bp, c), lane = threadIdx.x & 31;
+  if (!((route_mask >> j) & 1u)) return;
+  if (threadIdx.x < mp.D) s_load[threadIdx.x] = 0;
+  route_chunk(mp, bp, c, j, true, topk_idx, s_hist, [&](int t) { return route_scored<PL>(mp, rp, t, bp.layer[j], lane, logits + t * stride, topk_idx, topk_w); });
+  add_loads(mp, j, s_hist, s_load, mb_load, mb_cnt);
 }
 
 __global__ void route_clear_kernel(ModelParams mp, BatchParams bp, uint32_t route_mask, int32_t* mb_load,
@@ -63,7 +78,7 @@ bool ebi_router_ok(const eb_config& g, const eb_router* r, RouterParams* out, co
   return true;
 }
 
-// Clears the counts and routes; kind and router as in route_kernel.
+// Clears the counts and routes.  kind 0: softmax top-k on f32 logits, rows one behind the other; 1, 2: by the router, f32 or bf16 logits.
 static eb_status route_run(eb_ctx* c, void* stream, const eb_batch* batch, uint32_t route_mask, int kind, const RouterParams& rp, const void* logits,
                            int64_t stride, int32_t* topk_idx, float* topk_w, int32_t* mb_load, int32_t* mb_cnt) {
   BatchParams bp;
@@ -76,13 +91,19 @@ static eb_status route_run(eb_ctx* c, void* stream, const eb_batch* batch, uint3
   KernelTimer timer(c, EBK_ROUTE, st);
   int n = bp.n_mb * (c->cfg.E + c->cfg.D);
   EB_LAUNCH(c, "route", ebi_launch(route_clear_kernel, dim3((n + 255) / 256), dim3(256), 0, st, c->mp, bp, route_mask, mb_load, mb_cnt));
-  const bool few = c->cfg.E <= 64;
-  auto kernel = kind == 0   ? (few ? route_kernel<2, 0> : route_kernel<kMaxPerLane, 0>)
-                : kind == 1 ? (few ? route_kernel<2, 1> : route_kernel<kMaxPerLane, 1>)
-                            : (few ? route_kernel<2, 2> : route_kernel<kMaxPerLane, 2>);
-  if (bp.n_chunks > 0)
-    EB_LAUNCH(c, "route", ebi_launch(kernel, dim3(bp.n_chunks), dim3(kChunkThreads), 0, st, c->mp, bp, rp, route_mask, logits, stride, topk_idx, topk_w,
-                                     mb_load, mb_cnt));
+  if (bp.n_chunks > 0) {
+    const bool few = c->cfg.E <= 64;
+    const dim3 grid(bp.n_chunks), block(kChunkThreads);
+    if (kind == 0)
+      EB_LAUNCH(c, "route", ebi_launch(few ? route_kernel<2> : route_kernel<kMaxPerLane>, grid, block, 0, st, c->mp, bp, route_mask,
+                                       (const float*)logits, topk_idx, topk_w, mb_load, mb_cnt));
+    else if (kind == 1)
+      EB_LAUNCH(c, "route", ebi_launch(few ? route_scored_kernel<2, float> : route_scored_kernel<kMaxPerLane, float>, grid, block, 0, st, c->mp, bp, rp,
+                                       route_mask, (const float*)logits, stride, topk_idx, topk_w, mb_load, mb_cnt));
+    else
+      EB_LAUNCH(c, "route", ebi_launch(few ? route_scored_kernel<2, bf16> : route_scored_kernel<kMaxPerLane, bf16>, grid, block, 0, st, c->mp, bp, rp,
+                                       route_mask, (const bf16*)logits, stride, topk_idx, topk_w, mb_load, mb_cnt));
+  }
   EB_LAUNCH_CHECK(c, "route");
   return EB_OK;
 }
