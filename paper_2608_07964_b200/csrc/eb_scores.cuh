@@ -7,9 +7,10 @@
 // Order is what has to be exact: two c_e that differ by less than a rounding of 32 bits change places otherwise, and with them a
 // token's experts.  Without a bias c_e orders like z_e, so the logits are compared (integers in the order of the floats).  A sum, of a
 // bias or of two scores, is made and compared in 32 bits first, with a bound on how far it may be off: s_e = 1 / (1 + expf(-z)) is within 2^-21,
-// expf(z - top) / sum of at most 256 terms within 2^-19 (e^-d (d + 16) 2^-24, d = top - z), and the sum adds 2^-24 of its size.  Where neighbours of the
-// order, or the last group that stays and the first that goes, lie nearer than both bounds, the token is done again in 64 bits.
-// 65536 tokens, 256 experts in 8 groups: 389 us in 64 bits throughout, 205 this way.
+// expf(z - top) / sum of at most 256 terms within 2^-19 (e^-d (d + 16) 2^-24, d = top - z), and each sum adds 2^-24 of its size: c_e of its own, the
+// value of a group those of its two c_e as well, which with biases of opposite sign are larger than the value.  Where neighbours of the
+// order, or a group that stays and one that goes, lie nearer than both bounds, the token is done again in 64 bits.
+// 65536 tokens, 256 experts in 8 groups: 389 us in 64 bits throughout, 206 this way.
 #pragma once
 
 #include <cfloat>
@@ -41,10 +42,22 @@ __device__ __forceinline__ unsigned long long key_sum(unsigned long long a, unsi
   return b ? double_key(key_double(a) + key_double(b)) : a;
 }
 
+// The size of the terms of such a sum, of which each lacks up to 2^-24; 0 where there is no sum.
+__device__ __forceinline__ float term_size(unsigned a, unsigned b) { return b ? fabsf(key_float(a)) + fabsf(key_float(b)) : 0.f; }
+__device__ __forceinline__ float term_size(unsigned long long, unsigned long long) { return 0.f; }
+
 // Whether two values in 32 bits, the larger first, are sure to be in order: `off` is twice what either may be off by, whatever its size.
 __device__ __forceinline__ bool apart(float a, float b, float off) { return a - b > off + 0x1p-20f * (fabsf(a) + fabsf(b)); }
 __device__ __forceinline__ bool apart(unsigned a, unsigned b, float off) { return !b || apart(key_float(a), key_float(b), off); }
 __device__ __forceinline__ bool apart(unsigned long long, unsigned long long, float) { return true; }
+// Whether every group that stays is sure to be worth more than every one that goes.  value, terms: of group `lane` (0: none), its scores good to
+// off / 2.  A group has two of them, its sums lack up to 2^-24 of each term and of the value; 2^-20 leaves room for the roundings here.
+__device__ __forceinline__ bool groups_apart(unsigned value, float terms, bool kept, float off) {
+  const float v = key_float(value), e = off + 0x1p-20f * (fabsf(v) + terms), lo = v - e, hi = v + e;
+  const unsigned low = !kept ? 0xffffffffu : lo == lo ? float_key(lo) : 0u, high = kept || !value ? 0u : float_key(hi);
+  return __reduce_min_sync(0xffffffffu, low) > warp_max(high);
+}
+__device__ __forceinline__ bool groups_apart(unsigned long long, float, bool, float) { return true; }
 
 // Takes the best key of the warp: its value (0: none left) and, in *expert, the lowest index that has it; the holder's key is cleared.
 template <int PL, typename Key>
@@ -70,7 +83,8 @@ __device__ __forceinline__ Key take_best(Key (&key)[PL], int lane, int* expert) 
 template <int PL, typename Key>
 __device__ __forceinline__ bool keep_groups(const RouterParams& rp, int E, int lane, Key (&key)[PL], float off) {
   const int size = E / rp.n_group;
-  Key value = 0;   // lane g: of group g
+  Key value = 0;       // lane g: of group g
+  float terms = 0.f;   // of the sum that it is
   // a, b: the lane's best two of a group
   auto insert = [](Key k, Key& a, Key& b) {
     b = k > a ? a : k > b ? k : b;
@@ -78,13 +92,18 @@ __device__ __forceinline__ bool keep_groups(const RouterParams& rp, int E, int l
   };
   auto finish = [&](int g, Key a, Key b) {
     Key top = warp_max(a);
+    float both = 0.f;
     if (rp.group_top == 2) {
       // the holder (one of them) offers its second best
       const unsigned holders = __ballot_sync(0xffffffffu, a == top);
       const Key second = warp_max(lane == __ffs(holders) - 1 ? b : a);
+      both = term_size(top, second);
       top = top ? key_sum(top, second) : 0;
     }
-    if (lane == g) value = top;
+    if (lane == g) {
+      value = top;
+      terms = both;
+    }
   };
   if (size % 32 == 0) {   // whole registers of all lanes: those 65536 tokens took 265 us by the other way when they took 208 by this
     Key a = 0, b = 0;
@@ -111,16 +130,15 @@ __device__ __forceinline__ bool keep_groups(const RouterParams& rp, int E, int l
     }
   }
   unsigned kept = 0;
-  Key last = 0;
+  Key left_over = value;
   for (int n = 0; n < rp.topk_group; ++n) {
-    const Key top = warp_max(value);
+    const Key top = warp_max(left_over);
     if (!top) break;
-    const int g = __ffs(__ballot_sync(0xffffffffu, value == top)) - 1;
+    const int g = __ffs(__ballot_sync(0xffffffffu, left_over == top)) - 1;
     kept |= 1u << g;
-    if (lane == g) value = 0;
-    last = top;
+    if (lane == g) left_over = 0;
   }
-  const bool sure = !last || apart(last, warp_max(value), 2.f * off);
+  const bool sure = off <= 0.f || groups_apart(value, terms, (kept >> lane) & 1u, off);
   if (size % 32 == 0) {   // no divisions: a register holds experts of one group
     int left = size;
 #pragma unroll
