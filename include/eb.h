@@ -187,7 +187,8 @@ eb_status eb_route_scored(eb_ctx* ctx, void* stream, const eb_batch* batch, uint
                           int32_t* mb_load, int32_t* mb_cnt);
 
 /* From now on eb_route, eb_step and the calls around it gate by this router (copied; its bias is borrowed until the next
- * eb_set_router); NULL: by softmax top-k again, as after eb_create.  Graphs keep the router that they were captured with. */
+ * eb_set_router); NULL: by softmax top-k again, as after eb_create.  A graph keeps the router and the weights that were set and bound when it was
+ * captured: their memory (the bias, matrices, scales) is borrowed by it for as long as it is launched. */
 eb_status eb_set_router(eb_ctx* ctx, const eb_router* router);
 
 /* Schedule(S, m) of Algorithm 1 on the routed loads.  If the pool has at most m members all

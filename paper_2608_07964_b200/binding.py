@@ -244,6 +244,7 @@ class MoEStep:
             self.xs = raw[n:n + 4 * self.rows_cap * blocks].view(f32).view(self.rows_cap, blocks)
         self._weights = self._weights8 = self._router = None
         self._waited = 0          # ticket of the last schedule_wait
+        self.generation = 0       # counts the routers set and the weights bound: steps captured at another count are not what a step is now
 
     # -- helpers -------------------------------------------------------------------------------
     def _check(self, code: int, ctx="self"):
@@ -271,6 +272,7 @@ class MoEStep:
         assert tuple(w_gate.shape) == (self.L, self.E + self.S, self.I, self.H) == tuple(w_up.shape)
         assert tuple(w_down.shape) == (self.L, self.E + self.S, self.H, self.I)
         self._weights = (w_gate, w_up, w_down)
+        self.generation += 1
         self._check(self.lib.eb_bind_weights(self.ctx, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()))
 
     def quantize_weights(self, w: torch.Tensor):
@@ -294,13 +296,16 @@ class MoEStep:
         assert tuple(w_down.shape) == (self.L, n, self.H, self.I)
         assert tuple(s_gate.shape) == (self.L, n, ib, hb) == tuple(s_up.shape) and tuple(s_down.shape) == (self.L, n, hb, ib)
         self._weights8 = (w_gate, s_gate, w_up, s_up, w_down, s_down)
+        self.generation += 1
         self._check(self.lib.eb_bind_weights_fp8(self.ctx, *[t.data_ptr() for t in self._weights8]))
 
     def set_router(self, router: Optional[Router] = None):
-        """From now on eb_route and whole steps gate by `router`; None: by softmax top-k again."""
+        """From now on eb_route and whole steps gate by `router`; None: by softmax top-k again.  A graph that the caller captured keeps its router,
+        and with it the address of the bias: that tensor has to live as long as the graph (driver.StepGraphs captures anew instead)."""
         if router is not None and router.bias is not None:
             assert router.bias.device == self.logits.device and tuple(router.bias.shape) == (self.L, self.E)
         self._check(self.lib.eb_set_router(self.ctx, None if router is None else C.byref(router.c)))
+        self.generation += 1
         self._router = router   # its bias is borrowed
 
     # -- the five calls ------------------------------------------------------------------------

@@ -75,18 +75,24 @@ class StepGraphs:
     """CUDA graphs of whole steps, one per distinct (pool, layers, route mask, m, policy): a step's launches are
     fixed by those host-side values (which micro-batches run is read from device memory by the kernels), so a
     state that comes up again - the same schedule trajectory on the next batch - is replayed as one graph
-    launch instead of five or six kernel launches."""
+    launch instead of five or six kernel launches.  A graph holds the router and the weights of its step by address: once others are set
+    or bound (MoEStep.generation) it is dropped, and the step captured anew."""
 
     def __init__(self, step: "B.MoEStep", tok_off: List[int], capacity: int = 256):
         self.step, self.tok_off, self.capacity = step, list(tok_off), capacity
         self.graphs: Dict = {}
         self.hits = self.captures = 0
         self._last = 0            # ticket of the last step
+        self._generation = step.generation
 
     def run(self, layers: List[int], pool: int, route_mask: int, m: int, policy: int) -> int:
         """Launches the step; returns the ticket that its schedule is waited for with (MoEStep.schedule_wait), before the next step
         is launched.  A step launched without waiting for the one before may find that one's replay of the same graph, and so the same
         mark, still on its way: its ticket is then one that nothing marks, and the wait for it lasts until the step is over."""
+        if self._generation != self.step.generation:
+            torch.cuda.synchronize(self.step.dev)   # the last replay may still be on its way
+            self.graphs.clear()
+            self._generation = self.step.generation
         key = (pool, tuple(layers), route_mask, m, policy)
         g = self.graphs.get(key)
         if g is None:
