@@ -279,7 +279,8 @@ eb_status eb_permute_fp8(eb_ctx* ctx, void* stream, const eb_batch* batch, const
 
 /* eb_expert_ffn_grouped (device < 0; else eb_expert_ffn_device) on 8-bit rows and weights: products of e4m3 values summed in fp32 over
  * blocks of 128, the blocks' sums times both scales added up in fp32, silu(gate) * up quantised like a row (blocks of 128 of
- * the I outputs; one whose largest magnitude is below 2^-110 counts as zeros), yp bf16.  xq, xs: as eb_permute_fp8 leaves them. */
+ * the I outputs; one whose largest magnitude is below 2^-110 counts as zeros, and so does silu of a gate below -87), yp bf16.  xq, xs: as
+ * eb_permute_fp8 leaves them. */
 eb_status eb_expert_ffn_grouped_fp8(eb_ctx* ctx, void* stream, const void* xq, const float* xs, const int32_t* group_off,
                                     const int32_t* group_w, const int32_t* step_meta, void* yp, int32_t device);
 

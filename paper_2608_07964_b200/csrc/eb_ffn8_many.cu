@@ -42,6 +42,7 @@
 
 #include "eb_mma.cuh"
 #include "eb_quant.cuh"
+#include "eb_silu.cuh"
 #include "eb_tiles.cuh"
 
 namespace {
@@ -116,25 +117,6 @@ __device__ __forceinline__ float2 unpack2(uint64_t v) {
 }
 // two fp32 multiply-adds; volatile: they stay behind the wait for the TMEM loads that they take
 __device__ __forceinline__ void fma2(uint64_t& acc, uint64_t a, uint64_t b) { asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
-__device__ __forceinline__ float exp2f_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float rcp_approx(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// silu(g) * u for two values, sigmoid(g) = 1 / (1 + exp(-g)).  Not by tanh.approx: its 2^-11 would send one value in a hundred to
-// the other e4m3 neighbour.  The special function unit bounds the epilogue of a tile, so two quotients share one reciprocal: of the product, which
-// the exponents' limit of 2^60 keeps finite (a sigmoid below 2^-60 counts as that).
-__device__ __forceinline__ void silu_mul2(float g0, float u0, float g1, float u1, float* h0, float* h1) {
-  const float d0 = 1.f + exp2f_approx(fminf(g0 * -1.442695041f, 60.f)), d1 = 1.f + exp2f_approx(fminf(g1 * -1.442695041f, 60.f));
-  const float r = rcp_approx(d0 * d1);
-  *h0 = g0 * u0 * (r * d1);
-  *h1 = g1 * u1 * (r * d0);
-}
 
 struct TokenMaps8 {
   CUtensorMap box[5];   // 128 / 64 / 32 / 16 / 8 rows
