@@ -135,7 +135,7 @@ __device__ __forceinline__ void drain_packed(uint32_t acc, uint32_t (&out)[N][8]
     uint32_t a[P][16];
 #pragma unroll
     for (int k = 0; k < P; ++k) tmem_ld16(acc + kChunkStep * (i + k), a[k]);
-    tmem_ld_wait();
+    tmem_ld_wait(a);
 #pragma unroll
     for (int k = 0; k < P; ++k)
 #pragma unroll
@@ -212,14 +212,14 @@ __device__ __forceinline__ void epilogue_tile(const Tile& it, const TmemTurn& tu
     uint32_t r[NC][16];   // the gate accumulator; then outputs in [0..7]
 #pragma unroll
     for (int i = 0; i < NC; ++i) tmem_ld16(acc0 + kChunkStep * i, r[i]);
-    tmem_ld_wait();
+    tmem_ld_wait(r);
     if (turn.wide()) release_tmem(tempty0, lane);
 #pragma unroll
     for (int i = 0; i < 2 * NC; ++i) {   // eight columns at a time: no register is left for more
       uint32_t b[8];
       uint32_t* const g = r[i / 2] + (i % 2) * 8;
       tmem_ld8(acc1 + kChunkStep * (i / 2) + (i % 2) * 8, b);
-      tmem_ld_wait();
+      tmem_ld_wait(b);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         r[i / 2][(i % 2) * 4 + j] = pack_bf16(silu_mul(g[2 * j], b[2 * j]), silu_mul(g[2 * j + 1], b[2 * j + 1]));

@@ -77,12 +77,6 @@ __device__ __forceinline__ uint32_t instr_desc_e4m3(int n) { return (1u << 4) | 
 // Columns that a k-block of a tile takes per accumulator: 32, 64 or 128; a turn is 128 / width k-blocks.
 __device__ __forceinline__ int turn_width(int cols) { return cols <= 32 ? 32 : cols <= 64 ? 64 : 128; }
 
-// Waits for the thread's TMEM loads; the registers are named so that nothing reads them before.
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
-}
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
   uint64_t v;
   asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
@@ -141,7 +135,7 @@ __device__ __forceinline__ void add_block(Sums<NC>& s, uint32_t tmem, uint32_t s
 #pragma unroll
   for (int j = 0; j < 2 * NC; ++j) {
     const int a = j / NC, i = j % NC;
-    tmem_ld_wait16(r[j & 1]);
+    tmem_ld_wait(r[j & 1]);
     if (j + 1 < 2 * NC) tmem_ld16(tmem + ((j + 1) / NC) * width + 32 * ((j + 1) % NC), r[(j + 1) & 1]);
     const uint32_t at = scales + 4u * (a * width + 32 * i);
 #pragma unroll

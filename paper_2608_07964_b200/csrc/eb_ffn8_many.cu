@@ -115,7 +115,7 @@ __device__ __forceinline__ float2 unpack2(uint64_t v) {
   asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
   return make_float2(__uint_as_float(lo), __uint_as_float(hi));
 }
-// two fp32 multiply-adds; volatile: they stay behind the wait for the TMEM loads that they take
+// two fp32 multiply-adds; volatile: they stay in their order among the loads
 __device__ __forceinline__ void fma2(uint64_t& acc, uint64_t a, uint64_t b) { asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
 
 struct TokenMaps8 {
@@ -588,11 +588,11 @@ ffn8_many_kernel(const __grid_constant__ ManyParams p) {
           // 16 columns at a time, the next ones on their way while they are added; the last ones are added when the accumulator has been handed back
 #pragma unroll
           for (int i = 0; i < 2 * kEach - 1; ++i) {
-            tmem_ld_wait();
+            tmem_ld_wait(r[i & 1]);
             tmem_ld16(at + ((i + 1) / kEach) * 64 + ((i + 1) % kEach) * 16, r[(i + 1) & 1]);
             add_columns(sum[i / kEach] + i % kEach * 8, r[i & 1], i < kEach ? f0 : f1);
           }
-          tmem_ld_wait();
+          tmem_ld_wait(r[1]);
           tc_fence_before();
           if (stop) return false;
           bar_arrive(kBarRead, kGateThreads);
