@@ -244,6 +244,7 @@ class MoEStep:
             self.xs = raw[n:n + 4 * self.rows_cap * blocks].view(f32).view(self.rows_cap, blocks)
         self._weights = self._weights8 = self._router = None
         self._waited = 0          # ticket of the last schedule_wait
+        self.eight_bit = False    # the weights bound last are 8-bit ones
         self.generation = 0       # counts the routers set and the weights bound: steps captured at another count are not what a step is now
 
     # -- helpers -------------------------------------------------------------------------------
@@ -274,6 +275,7 @@ class MoEStep:
         self._weights = (w_gate, w_up, w_down)
         self.generation += 1
         self._check(self.lib.eb_bind_weights(self.ctx, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()))
+        self.eight_bit = False
 
     def quantize_weights(self, w: torch.Tensor):
         """bf16 matrices [..., rows, cols] as e4m3 values and f32 scales [..., ceil(rows / 128), ceil(cols / 128)]."""
@@ -298,6 +300,7 @@ class MoEStep:
         self._weights8 = (w_gate, s_gate, w_up, s_up, w_down, s_down)
         self.generation += 1
         self._check(self.lib.eb_bind_weights_fp8(self.ctx, *[t.data_ptr() for t in self._weights8]))
+        self.eight_bit = True
 
     def set_router(self, router: Optional[Router] = None):
         """From now on eb_route and whole steps gate by `router`; None: by softmax top-k again.  A graph that the caller captured keeps its router,

@@ -219,17 +219,18 @@ def idle_fractions(steps: List[Dict], D: int) -> Dict[str, float]:
 
 
 def device_times(step: "B.MoEStep", D: int, reps: int = 3) -> List[float]:
-    """Median time (ms) of the expert-pass kernels (gate/up and down)
+    """Median time (ms) of the expert-pass kernels (gate/up and down; of the weights bound last, on the rows of their dispatch)
     restricted to each virtual device's groups, from the library's per-kernel CUDA events; the tile-list
     construction that precedes them is not counted."""
     out = []
+    expert_pass = step.eb_expert_ffn_grouped_fp8 if step.eight_bit else step.eb_expert_ffn_grouped
     step.set_timing(True)
     try:
         for d in range(D):
-            step.eb_expert_ffn_grouped(device=d)                   # warm the path
+            expert_pass(device=d)                                  # warm the path
             ts = []
             for _ in range(reps):
-                step.eb_expert_ffn_grouped(device=d)
+                expert_pass(device=d)
                 k = step.kernel_ms()
                 ts.append(sum(v for name, v in k.items() if name.startswith(("ffn_gateup", "ffn_down"))))
             out.append(sorted(ts)[len(ts) // 2])
@@ -270,7 +271,7 @@ def run_emulated_latency(step: "B.MoEStep", tok_off: List[int], L: int, D: int, 
         else:
             batch = B.Batch(tok_off, lay, pool)
             run = step.eb_schedule(batch, m, policy, to_host=True)["run_mask"]
-        step.eb_permute(batch)
+        (step.eb_permute_fp8 if step.eight_bit else step.eb_permute)(batch)
         t = device_times(step, D)
         lat += max(t)
         busy += sum(t)
