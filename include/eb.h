@@ -101,7 +101,9 @@ typedef struct {
  *   best two (group_top 2; of one where there is only one); the topk_group best groups stay (ties: lower group first);
  *   the K best c_e of these are chosen, in that order (ties: lower index first), with weights scale * s_e, divided by the sum of
  *   the chosen s_e first if the context renormalises (renorm_topk).
- * Choices are made as by 64-bit scores: no near value is mistaken for a tie, or for the larger one.  A logit of -inf or NaN
+ * Choices are made as by 64-bit scores: no near value is mistaken for a tie, or for the larger one.  With a bias, or the sum of two, scores that are
+ * the same number in 64 bits tie: sigmoids of logits above 37 (all 1), softmax scores of logits 746 below the largest (all 0).  Without
+ * either the order of the scores is that of the logits, however near to 0 or 1 they come.  A logit of -inf or NaN
  * (and a bias of -inf or NaN) masks its expert: it is never chosen and counts for no group.  Slots for which no expert is left get
  * index -1 and weight 0: no row in the dispatch, nothing in the loads and in the aggregation.  A logit of +inf counts as the
  * largest float. */

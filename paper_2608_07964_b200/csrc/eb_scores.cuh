@@ -5,7 +5,8 @@
 //   the K best c_e of these groups; w = scale * s_e, over the sum of the chosen s_e if renormalised
 //
 // Order is what has to be exact: two c_e that differ by less than a rounding of 32 bits change places otherwise, and with them a
-// token's experts.  Without a bias c_e orders like z_e, so the logits are compared (integers in the order of the floats).  A sum, of a
+// token's experts.  Without a bias c_e orders like z_e, so the logits are compared (integers in the order of the floats), also where scores in 64 bits
+// would be 1 or 0 alike.  A sum, of a
 // bias or of two scores, is made and compared in 32 bits first, with a bound on how far it may be off: s_e = 1 / (1 + expf(-z)) is within 2^-21,
 // expf(z - top) / sum of at most 256 terms within 2^-19 (e^-d (d + 16) 2^-24, d = top - z), and each sum adds 2^-24 of its size: c_e of its own, the
 // value of a group those of its two c_e as well, which with biases of opposite sign are larger than the value.  Where neighbours of the
