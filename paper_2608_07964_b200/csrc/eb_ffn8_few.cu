@@ -22,8 +22,8 @@
 // The outputs of a CTA in a gate/up tile are one block of 128: its largest magnitudes per token are found by warp reductions and one
 // exchange between the four lane quadrants.  A down tile takes the scales that way from the workspace.
 //
-// What bounds it: with few rows the stream of weights (2048 rows over 191 matrices of 3 x 2048 x 1408, 1.65 GB: 302 us, 5.5 TB/s); with
-// many the issue of its MMAs, eight a k-block, and the ends of its tiles.
+// What bounds it: with few rows the stream of weights (2048 rows over 191 matrices of 3 x 2048 x 1408, 1.65 GB: 297 to 318 us pass after pass, 5.2
+// to 5.6 TB/s; 281 in bursts); with many the issue of its MMAs, eight a k-block, and the ends of its tiles.
 //
 // Every wait is bounded as in ffn_kernel.
 #include <cstddef>

@@ -12,9 +12,9 @@
 // That is why the TOKENS are the M operand here (256 rows a pair, 128 a CTA; a tile holds up to 256 rows) and 256 weight rows the N
 // operand: a TMEM lane is a token, so the product of both scales is one number per thread and block, the largest magnitude of a token's
 // outputs is found within threads, and a thread's outputs are neighbours in memory.  With the weights as M (eb_ffn8_few.cu) every
-// column has a scale of its own, which each thread reads from shared memory, and twice the MMAs have to be issued: 65536 rows over 66 matrices
-// of 3 x 2048 x 1408 take 924 us here and 1249 there, 8192 rows over 32 of 3 x 4096 x 14336 2680 and 3109; but 2048 rows over 191 of
-// 3 x 2048 x 1408 415 and 302, since a k-block costs much the same here however few its rows.
+// column has a scale of its own, which each thread reads from shared memory, and twice the MMAs have to be issued: in bursts of eight passes 65536
+// rows over 66 matrices of 3 x 2048 x 1408 take 807 us here and 1434 there, 8192 rows over 32 of 3 x 4096 x 14336 2342 and 3544; but 2048 rows
+// over 191 of 3 x 2048 x 1408 342 and 281, since a k-block costs much the same here however few its rows.  (eb_enable_fp8 has the border.)
 //
 // A gate/up tile makes 128 outputs: each CTA brings 64 rows of W_gate and the same 64 of W_up as its half of the N operand, so
 // that columns 0..63 | 64..127 of accumulator half c are gate | up of outputs 64 c ..; a down tile makes 256.  A thread
@@ -30,7 +30,7 @@
 // epilogue loop has nothing but one barrier, two words of scales, loads and multiply-adds in it; waits, scales and hand-overs are other
 // warps' work.  Measured on the way: waits by all lanes of all warps 170 cycles each, a wait with cluster scope by 32 lanes 6000, scales
 // fetched one block ahead 1000 a block, sixteen epilogue warps or waits within them no better, 32 columns a load worse (spills).
-// Multiply-adds are what the epilogue spends its time on: without them (wrong results) the 924 us are 684.
+// Multiply-adds are what the epilogue spends its time on: without them (wrong results) 65536 rows that took 924 us, pass after pass, took 684.
 //
 // A TMA box costs its issuing thread about 110 cycles, so token rows are one box (rounded up to a power of two: lanes without rows may hold
 // anything) or, in a merged tile, a box per lane.  The 128 outputs of a gate/up tile are a block of the intermediate: its largest magnitude per

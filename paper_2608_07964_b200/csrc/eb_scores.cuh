@@ -11,7 +11,7 @@
 // expf(z - top) / sum of at most 256 terms within 2^-19 (e^-d (d + 16) 2^-24, d = top - z), and each sum adds 2^-24 of its size: c_e of its own, the
 // value of a group those of its two c_e as well, which with biases of opposite sign are larger than the value.  Where neighbours of the
 // order, or a group that stays and one that goes, lie nearer than both bounds, the token is done again in 64 bits.
-// 65536 tokens, 256 experts in 8 groups: 389 us in 64 bits throughout, 206 this way.
+// 65536 tokens, 256 experts in 8 groups: 389 us in 64 bits throughout, 206 to 209 this way.
 #pragma once
 
 #include <cfloat>
